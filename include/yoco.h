@@ -18,6 +18,13 @@
  *   yoco_gret_prefill, yoco_gret_decode
  *                             gated retention (section 3.1, Eq. 4-7), chunkwise
  *                             for prompts and recurrent for generation
+ *   yoco_paged_append, yoco_paged_read, yoco_paged_attn
+ *                             a global cache in pages, bf16 or 4-bit codes:
+ *                             rows rotated to their positions and appended,
+ *                             read back, attended over
+ *   yoco_beam_select, yoco_beam_reorder_pages, yoco_beam_reorder_rows
+ *                             beam search: the best continuations, and page
+ *                             tables and states in their order
  *
  * Conventions
  *   - Every pointer named q/k/v/o/lens/workspace/mem is DEVICE memory owned by
@@ -65,7 +72,8 @@ typedef enum yoco_status {
 typedef enum yoco_dtype {
   YOCO_F32 = 0,
   YOCO_BF16 = 1,
-  YOCO_INT8 = 2 /* only as the dtype of a global cache, see below */
+  YOCO_INT8 = 2, /* only as the dtype of a global cache, see below */
+  YOCO_INT4 = 3  /* only as the dtype of a cache in pages, see there */
 } yoco_dtype;
 
 /*
@@ -405,6 +413,111 @@ int yoco_stack_step(const yoco_stack* st, const void* x, const yoco_kv_cache* ri
  * NULL: no addition, y unused), and h = swish(gu[:, :ffn]) * gu[:, ffn:] for gu [rows][2 ffn]. */
 int yoco_norm_rows(const void* x, const void* add, void* y, const void* gain, void* xn, int64_t rows, int dim, float eps, void* stream);
 int yoco_glu_rows(const void* gu, void* h, int64_t rows, int ffn, void* stream);
+
+/*
+ * ---- The global cache in pages ----
+ * A pool of pages of YOCO_PAGE_ROWS rows, and for every sequence a row of a table that says which page holds its rows
+ * 64 c .. 64 c + 63: table is int32 [B][cols] in device memory, so that a sequence holds up to 64 * cols rows. Sequences may
+ * share pages that neither of them writes any more (a common prompt). An entry outside [0, n_pages) stands for no page: its
+ * rows are not written, and read as if they were not there. Who has which page is the caller's to decide.
+ * Memory: the pages of K, then those of V, each [n_pages][Hkv][page of a head]. head_dim is 64 or 128. A page of a head, row r, dimension e:
+ *   YOCO_BF16, 128 d bytes. K element at ((r/16 * d/32 + e/32) * 64 + e/8 % 4 * 16 + r%16) * 8 + e%8
+ *                           V element at ((e/16 * 2 + r/32) * 64 + r%16 / 4 * 16 + e%16) * 8 + r/16 % 2 * 4 + r%4
+ *   YOCO_INT4, 36 d bytes.  K byte at (i/4 * 64 + e/8 % 4 * 16 + r%16) * 16 + i%4 * 4 + e%8 / 2 with i = r/16 * d/32 + e/32, nibble e%2
+ *                           V byte at (e/32 * 64 + r%16 / 4 * 16 + e%16) * 16 + r/16 * 4 + r%4, nibble e/16 % 2
+ *                           from byte 32 d on [64 rows][d/64] pairs of bf16: scale and minimum of dimensions 64 h .. 64 h + 63
+ * 4-bit coding, of 64 dimensions of a row and head at a time, all in float32 without fused products:
+ *   scale = bf16((max - min) * (1/15)), 0 below 2^-126;  base = bf16(min);  code = clamp(round-half-even((x - base) * (1/scale)), 0, 15)
+ * (scale 0: codes 0), and the value is base + scale * code. So a value is off by half a step of a fifteenth of its group's range, and by
+ * what bf16 rounds off the two. A group with an infinity or a NaN, or whose range is none, reads as NaN. 4.5 bits a value: 0.28 times the bytes of bf16.
+ */
+#define YOCO_PAGE_ROWS 64
+
+typedef struct yoco_paged_cache {
+  void* k;          /* device: pages of K */
+  void* v;          /* device: pages of V */
+  int32_t n_pages;
+  int32_t Hkv;
+  int32_t d;        /* 64 or 128 */
+  int32_t dtype;    /* YOCO_BF16 or YOCO_INT4 */
+} yoco_paged_cache;
+
+/* Bytes of a pool, and its description over `mem` (device memory, 256-byte aligned). Host only; the memory is not touched. */
+int yoco_paged_cache_bytes(int n_pages, int Hkv, int d, int dtype, size_t* bytes);
+int yoco_paged_cache_init(void* mem, size_t bytes, int n_pages, int Hkv, int d, int dtype, yoco_paged_cache* out);
+
+/*
+ * Rotation to positions: the first `dims` dimensions of a head (a multiple of 16) are dims / 2 pairs, dimension p with
+ * p + dims / 2, or 2 p with 2 p + 1 where neighbours != 0. A pair (x, y) at position n becomes (x cos a - y sin a, y cos a + x sin a).
+ * Its angle is given as turns[p], what a step of one position turns it by, in 2^-64 of a full turn (device memory): n * turns[p],
+ * wrapped to 64 bits, is exact at any position, where a product of float32 numbers is off by 0.03 at position 524288. The angle
+ * is the upper 32 bits of that, as a signed number, in float32 radians.
+ */
+typedef struct yoco_rotation {
+  const uint64_t* turns; /* device: [dims / 2] */
+  int32_t dims;
+  int32_t neighbours;
+} yoco_rotation;
+
+/*
+ * Append rows: row t of sequence b, t < T (t < rows[b] where rows, device int64 [B], is given), goes to position pos[b] + t
+ * (pos: device int64 [B]). k and v have rows of Hkv * d elements `k_stride` and `v_stride` elements apart, row b * T + t for that
+ * one, of `src_dtype` (YOCO_F32, YOCO_BF16); k is rotated (rotation: or NULL), then both are rounded or coded. q (or NULL): rows of Hq * d elements
+ * q_stride apart, all T of a sequence, rotated likewise into q_out, dense [B][T][Hq][d] of the same type; q_out == q is allowed where q is dense.
+ * Strides are multiples of 8 elements. A row at a position that the table has no page for is not written; two rows of a call must not
+ * meet in one place. T == 0 is a no-op.
+ */
+int yoco_paged_append(const yoco_paged_cache* c, const int32_t* table, int B, int cols, const int64_t* pos, const int64_t* rows, int64_t T, const void* k,
+                      int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int Hq, const yoco_rotation* rotation,
+                      int src_dtype, void* stream);
+
+/* The values of rows pos[b] .. pos[b] + T - 1, into k and v: dense [B][T][Hkv][d] of dst_dtype (YOCO_F32, YOCO_BF16: rounded
+ * once); zeros where the table has no page. T == 0 is a no-op. */
+int yoco_paged_read(const yoco_paged_cache* c, const int32_t* table, int B, int cols, const int64_t* pos, int64_t T, void* k, void* v, int dst_dtype, void* stream);
+
+/*
+ * Eq. 3 over the pages for the last T rows of every sequence: row i of T is at position lens[b] - T + i and attends to the rows up to
+ * itself. q, o: bf16 [B][T][Hq][d]; lens: device int64 [B], clamped to [0, 64 * cols]; a row before position 0 gets zeros, and so
+ * does one for whose rows the table has no page. T == 0 is a no-op. Rows of K and V that are attended to must be finite numbers for a finite result.
+ * workspace: at least yoco_paged_attn_workspace() bytes, 16-byte aligned; needs no clearing; calls that overlap in time must not share it.
+ */
+int yoco_paged_attn_workspace(const yoco_paged_cache* c, int B, int cols, int T, int Hq, size_t* bytes);
+int yoco_paged_attn(const yoco_paged_cache* c, const int32_t* table, int B, int cols, const void* q, void* o, const int64_t* lens, int T, int Hq, float scale,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- Beam search ----
+ * B requests of W beams (up to YOCO_MAX_BEAMS) each; beam w of request b is row b * W + w of whatever has a row a beam.
+ */
+#define YOCO_MAX_BEAMS 16
+
+/*
+ * The W best continuations of every request. Candidates are (beam w, token t) with the score scores[b][w] + (x - lse), x the
+ * beam's logit of t and lse the logarithm of the sum of exp over its logits, in float32. Logits of -infinity and NaN are no candidates, and
+ * add nothing to lse; +infinity counts as the largest number. A beam with done[b][w] != 0 (done: or NULL) has one candidate, (w, eos) with its score as it
+ * is, and its logits are not read; a score of -infinity or NaN leaves a beam without candidates. Order: the higher score, then the lower beam, then the
+ * higher logit, then the lower token. parent, token, scores_out [B][W] and done_out (or NULL; done of the parent, or token == eos)
+ * get the best, best first; where fewer are left, place w gets parent w, token eos (0 for eos < 0) and -infinity. eos < 0: no token ends a beam.
+ * logits: [B * W] rows of V elements `stride` apart (>= V), YOCO_F32 or YOCO_BF16. V is at most 524288. No output may be an input.
+ */
+int yoco_beam_select_workspace(int B, int W, int V, size_t* bytes);
+int yoco_beam_select(const void* logits, int64_t stride, const float* scores, const uint8_t* done, int eos, int B, int W, int V, int dtype, int32_t* parent,
+                     int32_t* token, float* scores_out, uint8_t* done_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Beams in the order of their parents, over a cache in pages. Every beam has pages of its own, home [B * W][cols], of which no two are the
+ * same; table [B * W][cols] says where its rows are: in pages of its prompt, of other beams, and of its own. lens: device int64 [B * W], the
+ * rows that a beam has (the same for all beams of a request; the first one's is read). Beam w takes over the table of beam parent[b][w]; the page
+ * that its next row goes to becomes its own (column lens / 64), with what the parent's page of that column holds. So pages are shared once they are full, and a
+ * beam only ever writes to its own. A parent outside [0, W) leaves the beam as it is. Before a first row is appended behind a
+ * prompt that all beams share, a call with parent[b][w] = w gives each its own copy of the page that the prompt ends in.
+ */
+int yoco_beam_reorder_pages(const yoco_paged_cache* c, int32_t* table, const int32_t* home, int B, int W, int cols, const int32_t* parent, const int64_t* lens,
+                            void* stream);
+
+/* Other states, in place: each of the n buffers is [B][W] rows of row_bytes[i] bytes (a multiple of 16), and row (b, w) becomes what
+ * row (b, parent[b][w]) was: planes of rolling caches, retention states, residual streams. mem and row_bytes are host arrays; buffers must not overlap. */
+int yoco_beam_reorder_rows(void* const* mem, const int64_t* row_bytes, int n, int B, int W, const int32_t* parent, void* stream);
 
 /*
  * ---- Measured ceilings (measurement aids for the benchmark, not part of the path) ----

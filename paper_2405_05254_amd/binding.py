@@ -2,11 +2,13 @@
 ctypes; the calls of a running model are checked and marshalled in native code (csrc/py_calls.cpp), because a step over a
 small cache or state takes no longer than Python took to check its arguments."""
 import ctypes as C
+import math
 import os
 
 import torch
 
-F32, BF16, INT8 = 0, 1, 2
+F32, BF16, INT8, INT4 = 0, 1, 2, 3
+PAGE_ROWS = 64
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 _CALLS = None
@@ -30,6 +32,14 @@ class _Stack(C.Structure):
 class _Cache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("B", C.c_int32), ("Hkv", C.c_int32),
                 ("d", C.c_int32), ("dtype", C.c_int32), ("N_cap", C.c_int64)]
+
+
+class _Paged(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32)]
+
+
+class _Rotation(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("dims", C.c_int32), ("neighbours", C.c_int32)]
 
 
 def lib_path():
@@ -70,6 +80,16 @@ def lib():
     L.yoco_stack_step.argtypes = [C.POINTER(_Stack), vp, C.POINTER(_Cache), C.POINTER(vp), C.POINTER(_Cache), i64, vp, vp, vp, sz, vp, sz, vp]
     L.yoco_norm_rows.argtypes = [vp, vp, vp, vp, vp, i64, i32, f32, vp]
     L.yoco_glu_rows.argtypes = [vp, vp, i64, i32, vp]
+    L.yoco_paged_cache_bytes.argtypes = [i32, i32, i32, i32, C.POINTER(sz)]
+    L.yoco_paged_cache_init.argtypes = [vp, sz, i32, i32, i32, i32, C.POINTER(_Paged)]
+    L.yoco_paged_append.argtypes = [C.POINTER(_Paged), vp, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, C.POINTER(_Rotation), i32, vp]
+    L.yoco_paged_read.argtypes = [C.POINTER(_Paged), vp, i32, i32, vp, i64, vp, vp, i32, vp]
+    L.yoco_paged_attn_workspace.argtypes = [C.POINTER(_Paged), i32, i32, i32, i32, C.POINTER(sz)]
+    L.yoco_paged_attn.argtypes = [C.POINTER(_Paged), vp, i32, i32, vp, vp, vp, i32, i32, f32, vp, sz, vp]
+    L.yoco_beam_select_workspace.argtypes = [i32, i32, i32, C.POINTER(sz)]
+    L.yoco_beam_select.argtypes = [vp, i64, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.yoco_beam_reorder_pages.argtypes = [C.POINTER(_Paged), vp, vp, i32, i32, i32, vp, vp, vp]
+    L.yoco_beam_reorder_rows.argtypes = [C.POINTER(vp), C.POINTER(i64), i32, i32, i32, vp, vp]
     L.yoco_ceiling_mfma.argtypes = [vp, vp, i32, i32, vp]
     L.yoco_ceiling_attn_loop.argtypes = [vp, vp, i32, i32, i32, vp]
     L.yoco_ceiling_stream_read.argtypes = [vp, sz, vp, i32, vp]
@@ -77,7 +97,9 @@ def lib():
                  "yoco_cross_attn_prefill", "yoco_cross_attn_prefill_workspace", "yoco_cross_attn_decode_workspace", "yoco_cross_attn_decode", "yoco_cross_attn_decode_noalloc",
                  "yoco_swa_cache_write", "yoco_kv_cache_append", "yoco_swa_decode",
                  "yoco_gret_prefill_workspace", "yoco_gret_prefill", "yoco_gret_decode",
-                 "yoco_stack_step_scratch", "yoco_stack_step", "yoco_norm_rows", "yoco_glu_rows"):
+                 "yoco_stack_step_scratch", "yoco_stack_step", "yoco_norm_rows", "yoco_glu_rows",
+                 "yoco_paged_cache_bytes", "yoco_paged_cache_init", "yoco_paged_append", "yoco_paged_read", "yoco_paged_attn_workspace", "yoco_paged_attn",
+                 "yoco_beam_select_workspace", "yoco_beam_select", "yoco_beam_reorder_pages", "yoco_beam_reorder_rows"):
         getattr(L, name).restype = i32
     _LIB = L
     return L
@@ -321,6 +343,88 @@ def glu_rows(gu):
         return h
     _check(lib().yoco_glu_rows(_dev(gu, "gu"), _dev(h, "h"), h.shape[0], h.shape[1], _stream()))
     return h
+
+
+class PagedCache:
+    """A pool of pages of 64 rows (yoco_paged_cache), bf16 or 4-bit codes (dtype INT4): torch owns the memory. Which sequence
+    has which pages is the program's, in int32 tables [B, columns] on the device. mem: memory to describe, else it is allocated."""
+
+    def __init__(self, n_pages, Hkv, d, dtype=torch.bfloat16, device="cuda", mem=None):
+        if dtype not in (torch.bfloat16, INT4):
+            raise YocoError("a cache in pages is torch.bfloat16 or INT4, not %s" % (dtype,))
+        code = INT4 if dtype == INT4 else BF16
+        n = C.c_size_t()
+        _check(lib().yoco_paged_cache_bytes(n_pages, Hkv, d, code, C.byref(n)))
+        self.bytes = n.value
+        self.mem = torch.empty(self.bytes, dtype=torch.uint8, device=device) if mem is None else mem
+        self.desc = _Paged()
+        _check(lib().yoco_paged_cache_init(_dev(self.mem, "mem"), self.mem.numel() * self.mem.element_size(), n_pages, Hkv, d, code, C.byref(self.desc)))
+        self.n_pages, self.Hkv, self.d, self.dtype = n_pages, Hkv, d, dtype
+
+    @property
+    def address(self):
+        return C.addressof(self.desc)
+
+
+def rotation_turns(dims, base=10000.0, device="cuda"):
+    """int64 [dims / 2]: what a position turns pair p by, base^(-2 p / dims) radians, in 2^-64 of a full turn (yoco_rotation). For
+    other frequencies: turn_units of their angles."""
+    return turn_units([base ** (-2.0 * p / dims) for p in range(dims // 2)], device)
+
+
+def turn_units(radians, device="cuda"):
+    """int64 tensor of angles in 2^-64 of a full turn, wrapped to the signed range (yoco_rotation)."""
+    units = [int(round(a / (2.0 * math.pi) * 2.0 ** 64)) % 2 ** 64 for a in radians]
+    return torch.tensor([u - 2 ** 64 if u >= 2 ** 63 else u for u in units], dtype=torch.int64, device=device)
+
+
+def paged_append(cache, table, pos, k, v, rows=None, q=None, turns=None, neighbours=False, q_out=None):
+    """k, v [B,T,Hkv,d] (float32 or bfloat16; rows may be apart, as in views of a joined product) -> rows pos[b] .. of the pages that
+    table int32 [B,columns] names; rows int64 [B]: how many of the T are new (None: all). With turns (rotation_turns) k is rotated to its
+    positions, and q [B,T,Hq,d] too, which is returned (yoco_paged_append)."""
+    return (_CALLS or _calls()).paged_append(cache.address, table, pos, k, v, rows, q, turns, neighbours, q_out)
+
+
+def paged_read(cache, table, pos, T, dtype=torch.bfloat16):
+    """The values of rows pos[b] .. pos[b] + T - 1: k, v [B,T,Hkv,d] (yoco_paged_read)."""
+    k, v = (torch.empty((table.shape[0], T, cache.Hkv, cache.d), dtype=dtype, device=table.device) for _ in range(2))
+    (_CALLS or _calls()).paged_read(cache.address, table, pos, T, k, v)
+    return k, v
+
+
+def paged_attn_workspace(cache, B, columns, T, Hq):
+    n = C.c_size_t()
+    _check(lib().yoco_paged_attn_workspace(C.byref(cache.desc), B, columns, T, Hq, C.byref(n)))
+    return n.value
+
+
+def paged_attn(cache, table, q, lens, scale, workspace=None, out=None):
+    """q bfloat16 [B,T,Hq,d], the last T rows of sequences of lens int64 [B] rows -> o, causal over the pages (yoco_paged_attn).
+    workspace: device tensor of paged_attn_workspace bytes; None: taken from torch's allocator."""
+    return (_CALLS or _calls()).paged_attn(cache.address, table, q, lens, scale, workspace, out)
+
+
+def beam_select_workspace(B, W, V):
+    n = C.c_size_t()
+    _check(lib().yoco_beam_select_workspace(B, W, V, C.byref(n)))
+    return n.value
+
+
+def beam_select(logits, scores, done=None, eos=-1, workspace=None):
+    """logits [B,W,V] (float32 or bfloat16), scores float32 [B,W], done bool [B,W] -> parent, token int32, scores float32, done bool
+    [B,W], the W best continuations of each request, best first (yoco_beam_select)."""
+    return (_CALLS or _calls()).beam_select(logits, scores, done, eos, workspace)
+
+
+def beam_reorder_pages(cache, table, home, parent, lens):
+    """table int32 [B*W,columns] in place in the order of parent int32 [B,W]; the page that the next row goes to becomes the beam's
+    own (home, like table) with the parent's content; lens int64 [B*W] (yoco_beam_reorder_pages)."""
+    (_CALLS or _calls()).beam_reorder_pages(cache.address, table, home, parent, lens)
+
+
+def beam_reorder_rows(states, parent):
+    """Tensors [B*W, ...] in place: row (b, w) becomes what row (b, parent[b, w]) was (yoco_beam_reorder_rows)."""
+    (_CALLS or _calls()).beam_reorder_rows(states, parent)
 
 
 def ceiling_mfma(seed, sink, iters, workgroups):

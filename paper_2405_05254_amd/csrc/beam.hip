@@ -1,0 +1,338 @@
+// Beam search: the best continuations of a request's beams over the vocabulary, and the states of the beams put in the
+// order that follows from them.
+//
+// Selection. Within a beam score + logit - log-sum-exp grows with the logit, so a beam's W best logits are all that can be
+// chosen of it: one pass over the logits keeps, of every chunk, the maximum, the sum of exponentials and the W best, and what
+// is left is small. Candidates of a beam are ordered by logit and then token, candidates of a request by score and then beam.
+#include "decode_tail.h"
+#include "paged.h"
+
+namespace yoco {
+
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMaxBeams = 16;
+
+// Larger numbers for better candidates: the logit's bits in an order that unsigned numbers have, then the smaller token.
+__device__ __forceinline__ unsigned ordered(float x) {
+  const unsigned u = __float_as_uint(x);
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(unsigned u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
+__device__ __forceinline__ uint64_t key_of(float x, int token) { return (uint64_t)ordered(x) << 32 | (unsigned)~token; }
+constexpr uint64_t kNoKey = 0;            // below every candidate: no logit has these bits but a NaN
+
+__device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane) {
+  return (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)k, lane);
+}
+
+// The W best of a wavefront's keys, N a lane, best first, into `best`; kNoKey where there are fewer. `list` holds W * N keys. Every lane's best
+// one is ranked among the 64: the W-th of those bounds the W-th of all from below, and only W lanes can hold any above it.
+template <int N>
+__device__ __forceinline__ void wave_best(const uint64_t (&k)[N], int W, uint64_t* list, uint64_t* best) {
+  const int lane = threadIdx.x & 63;
+  uint64_t mine = k[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) mine = k[i] > mine ? k[i] : mine;
+  int rank = 0;
+  for (int j = 0; j < 64; ++j) {
+    const uint64_t other = lane_key(mine, j);
+    rank += other > mine || (other == mine && j < lane);
+  }
+  const uint64_t least = lane_key(mine, __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == W - 1)));
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint64_t in = __builtin_amdgcn_ballot_w64(k[i] >= least && k[i] != kNoKey);
+    if (k[i] >= least && k[i] != kNoKey) list[n + __builtin_amdgcn_mbcnt_hi((unsigned)(in >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in, 0))] = k[i];
+    n += __builtin_popcountll(in);
+  }
+  if (lane < W) best[lane] = kNoKey;
+  __builtin_amdgcn_wave_barrier();
+  for (int i = lane; i < n; i += 64) {
+    const uint64_t key = list[i];
+    int r = 0;
+    for (int j = 0; j < n; ++j) r += list[j] > key;
+    if (r < W) best[r] = key;
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// 8 logits from element `at` on, those outside [lo, hi) as -inf. `at` is a multiple of 8 and `end` the number of elements that there are.
+__device__ __forceinline__ void logits8(const float* p, int64_t at, int64_t end, float (&x)[8]) {
+  if (at + 8 <= end) {
+    const f32x4 a = *(const f32x4*)(p + at), b = *(const f32x4*)(p + at + 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[j] = a[j];
+      x[4 + j] = b[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = at + j < end ? p[at + j] : 0.f;
+  }
+}
+__device__ __forceinline__ void logits8(const bf16_t* p, int64_t at, int64_t end, float (&x)[8]) {
+  if (at + 8 <= end) {
+    const u32x4 a = *(const u32x4*)(p + at);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(a[j] << 16);
+      x[2 * j + 1] = __uint_as_float(a[j] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = at + j < end ? bf16_to_f32(p[at + j]) : 0.f;
+  }
+}
+
+__device__ __forceinline__ float sum_exp(float m, float from, float sum) {       // a sum relative to `from`, relative to m >= from
+  return from == -INFINITY ? 0.f : sum * __expf(from - m);
+}
+
+// What a chunk leaves: maximum and sum of exponentials (two floats), then its W best keys.
+__host__ __device__ inline size_t chunk_words(int W) { return 1 + (size_t)W; }     // of 64 bits
+
+template <typename S, int VECS>           // 8-logit pieces a thread
+__global__ void __launch_bounds__(256) select_chunks_kernel(SelectView a, uint64_t* ws) {
+  __shared__ uint64_t list[4][kMaxBeams * VECS * 8], best[4][kMaxBeams];
+  __shared__ float stats[4][2];
+  const int row = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, W = a.W;
+  if (a.done && a.done[row]) return;
+  const int64_t first = (int64_t)row * a.stride, last = first + a.V, end = (int64_t)(a.B * W - 1) * a.stride + a.V;
+  const int64_t v0 = first / 8 + (int64_t)blockIdx.x * (VECS * 256) + threadIdx.x;
+  uint64_t k[VECS * 8];
+  float m = -INFINITY, l = 0.f, x[VECS * 8];
+#pragma unroll
+  for (int i = 0; i < VECS; ++i) {
+    const int64_t at = (v0 + i * 256) * 8;
+    float y[8] = {};
+    if (at < last) logits8((const S*)a.logits, at, end, y);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      // a NaN is no candidate, and an infinity the largest number
+      const bool in = at + j >= first && at + j < last && !is_nan(y[j]) && y[j] != -INFINITY;
+      const float z = in ? fminf(y[j], 3.402823466e38f) : -INFINITY;
+      x[i * 8 + j] = z;
+      m = fmaxf(m, z);
+      k[i * 8 + j] = in ? key_of(z, (int)(at + j - first)) : kNoKey;
+    }
+  }
+  m = over64<LaneMax>(m);
+  if (m > -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < VECS * 8; ++i) l += __expf(x[i] - m);
+  }
+  l = over64<LaneSum>(l);
+  wave_best(k, W, list[wave], best[wave]);
+  if (lane == 0) {
+    stats[wave][0] = m;
+    stats[wave][1] = l;
+  }
+  __syncthreads();
+  if (wave) return;
+  uint64_t* const out = ws + ((size_t)row * gridDim.x + blockIdx.x) * chunk_words(W);
+  const uint64_t mine[1] = {lane < 4 * W ? best[lane / W][lane % W] : kNoKey};
+  wave_best(mine, W, list[0], best[0]);
+  if (lane < W) out[1 + lane] = best[0][lane];
+  if (lane == 0) {
+    const float M = fmaxf(fmaxf(stats[0][0], stats[1][0]), fmaxf(stats[2][0], stats[3][0]));
+    float sum = 0.f;
+    for (int w = 0; w < 4; ++w) sum += sum_exp(M, stats[w][0], stats[w][1]);
+    out[0] = (uint64_t)__float_as_uint(sum) << 32 | __float_as_uint(M);
+  }
+}
+
+constexpr int kMaxChunks = 65;            // a row that starts inside a piece of 8 reaches into one chunk more than 64
+constexpr int kMergeKeys = (kMaxChunks * kMaxBeams + 63) / 64;
+
+// A request's candidates from those of its beams' chunks.
+__global__ void __launch_bounds__(256) select_merge_kernel(SelectView a, const uint64_t* ws, int chunks) {
+  __shared__ uint64_t list[4][kMaxBeams * kMergeKeys], best[kMaxBeams][kMaxBeams];
+  __shared__ float lse[kMaxBeams], score[kMaxBeams * kMaxBeams];
+  const int b = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, W = a.W;
+  for (int w = wave; w < W; w += 4) {
+    const int row = b * W + w;
+    if (a.done && a.done[row]) continue;
+    const uint64_t* const p = ws + (size_t)row * chunks * chunk_words(W);
+    float m = -INFINITY, l = 0.f;
+    for (int c = lane; c < chunks; c += 64) {
+      const uint64_t x = p[c * chunk_words(W)];
+      const float mc = __uint_as_float((unsigned)x), M = fmaxf(m, mc);
+      l = sum_exp(M, m, l) + sum_exp(M, mc, __uint_as_float((unsigned)(x >> 32)));
+      m = M;
+    }
+    const float M = over64<LaneMax>(m);
+    l = over64<LaneSum>(sum_exp(M, m, l));
+    uint64_t k[kMergeKeys];
+#pragma unroll
+    for (int i = 0; i < kMergeKeys; ++i) {
+      const int j = i * 64 + lane, c = j / W;
+      k[i] = c < chunks ? p[c * chunk_words(W) + 1 + j % W] : kNoKey;
+    }
+    wave_best(k, W, list[wave], best[w]);
+    if (lane == 0) lse[w] = M + logf(l);
+  }
+  __syncthreads();
+  // a candidate a thread, in the order that decides between equal scores
+  const int t = threadIdx.x, w = t / W, r = t % W;
+  float mine = -INFINITY;
+  int token = a.eos >= 0 ? a.eos : 0;
+  if (w < W) {
+    const float base = a.scores[b * W + w];
+    if (a.done && a.done[b * W + w]) {
+      if (r == 0) mine = base;
+    } else if (best[w][r] != kNoKey) {
+      token = (int)~(unsigned)best[w][r];
+      mine = base + (unordered((unsigned)(best[w][r] >> 32)) - lse[w]);
+    }
+    if (is_nan(mine)) mine = -INFINITY;
+    score[t] = mine;
+  }
+  __syncthreads();
+  if (w >= W) return;
+  int rank = 0;
+  for (int j = 0; j < W * W; ++j) rank += score[j] > mine || (score[j] == mine && j < t);
+  if (rank >= W) return;
+  const int out = b * W + rank;
+  const bool none = mine == -INFINITY;                                // no candidate is left: the place stays its own beam's
+  const int parent = none ? rank : w;
+  if (none) token = a.eos >= 0 ? a.eos : 0;
+  a.parent[out] = parent;
+  a.token[out] = token;
+  a.scores_out[out] = mine;
+  if (a.done_out) a.done_out[out] = (a.done && a.done[b * W + parent]) || token == a.eos;
+}
+
+// 8-logit pieces a thread so that the chunks are few enough to be merged by one wavefront and enough to fill the chip.
+int select_pieces(int rows, int V) {
+  for (int vecs = 1; vecs < 4; vecs *= 2)
+    if ((V + 2048 * vecs - 1) / (2048 * vecs) <= 32 && (int64_t)rows * V <= (int64_t)2048 * vecs * 1024) return vecs;
+  return 4;
+}
+int select_chunks(int vecs, int V) { return ((V + 7) / 8 + 1 + vecs * 256 - 1) / (vecs * 256); }     // of a row that starts anywhere
+
+// ---- states in the order of their parents, in place: a thread has the same 16 bytes of all beams, and reads before it writes
+template <int WM>
+__device__ __forceinline__ void reorder_piece(u32x4* p, int64_t stride, int W, const int (&from)[WM]) {
+  u32x4 x[WM];
+#pragma unroll
+  for (int w = 0; w < WM; ++w)
+    if (w < W && from[w] != w) x[w] = p[from[w] * stride];
+#pragma unroll
+  for (int w = 0; w < WM; ++w)
+    if (w < W && from[w] != w) p[w * stride] = x[w];
+}
+// A parent that is none of the request's beams leaves the beam as it is.
+template <int WM>
+__device__ __forceinline__ void parents_of(const int32_t* parent, int b, int W, int (&from)[WM]) {
+#pragma unroll
+  for (int w = 0; w < WM; ++w) {
+    const int p = parent[b * W + (w < W ? w : 0)];
+    from[w] = p >= 0 && p < W ? p : w;
+  }
+}
+
+template <int WM>
+__global__ void __launch_bounds__(256) reorder_rows_kernel(ReorderRows r, int W, const int32_t* parent) {
+  const int b = blockIdx.y, z = blockIdx.z;
+  int from[WM];
+  parents_of<WM>(parent, b, W, from);
+  const int64_t n = r.pieces[z];
+  u32x4* const base = (u32x4*)r.mem[z] + (int64_t)b * W * n;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) reorder_piece<WM>(base + i, n, W, from);
+}
+
+// The page that the next row goes to: its content comes from the parent's into the beam's own.
+template <int WM>
+__global__ void __launch_bounds__(256) reorder_tail_kernel(yoco_paged_cache c, const int32_t* table, const int32_t* home, int W, int cols, const int32_t* parent, const int64_t* lens) {
+  const int b = blockIdx.y;
+  const int64_t len = lens[(int64_t)b * W], tail = len / kPageRows;
+  if (len <= 0 || len % kPageRows == 0 || tail >= cols) return;
+  int from[WM];
+  parents_of<WM>(parent, b, W, from);
+  const int64_t n = (int64_t)c.Hkv * page_bytes(c.d, c.dtype) / 16;
+  u32x4* const plane = (u32x4*)(blockIdx.z ? c.v : c.k);
+  int64_t source[WM], into[WM];
+#pragma unroll
+  for (int w = 0; w < WM; ++w) {
+    const int64_t row = (int64_t)b * W;
+    const int s = table[(row + from[w < W ? w : 0]) * cols + tail], h = home[(row + (w < W ? w : 0)) * cols + tail];
+    const bool moves = w < W && s != h && s >= 0 && s < c.n_pages && h >= 0 && h < c.n_pages;
+    source[w] = moves ? s * n : 0;
+    into[w] = moves ? h * n : -1;
+  }
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    u32x4 x[WM];
+#pragma unroll
+    for (int w = 0; w < WM; ++w)
+      if (into[w] >= 0) x[w] = plane[source[w] + i];
+#pragma unroll
+    for (int w = 0; w < WM; ++w)
+      if (into[w] >= 0) plane[into[w] + i] = x[w];
+  }
+}
+
+template <int WM>
+__global__ void __launch_bounds__(256) reorder_table_kernel(int32_t* table, const int32_t* home, int W, int cols, const int32_t* parent, const int64_t* lens) {
+  const int b = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= cols) return;
+  int from[WM], x[WM];
+  parents_of<WM>(parent, b, W, from);
+  const int64_t len = lens[(int64_t)b * W], row = (int64_t)b * W;
+  const bool own = i == (len > 0 ? len / kPageRows : 0);
+#pragma unroll
+  for (int w = 0; w < WM; ++w)
+    if (w < W) x[w] = own ? home[(row + w) * cols + i] : table[(row + from[w]) * cols + i];
+#pragma unroll
+  for (int w = 0; w < WM; ++w)
+    if (w < W) table[(row + w) * cols + i] = x[w];
+}
+
+template <typename F>
+void by_beams(int W, F f) {
+  if (W <= 4) f(std::integral_constant<int, 4>());
+  else if (W <= 8) f(std::integral_constant<int, 8>());
+  else f(std::integral_constant<int, kMaxBeams>());
+}
+
+}  // namespace
+
+size_t beam_select_workspace(int B, int W, int V) { return (size_t)B * W * select_chunks(select_pieces(B * W, V), V) * chunk_words(W) * sizeof(uint64_t); }
+
+hipError_t launch_beam_select(const SelectView& a, int dtype, void* workspace, hipStream_t s) {
+  const int rows = a.B * a.W, vecs = select_pieces(rows, a.V), chunks = select_chunks(vecs, a.V);
+  const dim3 grid(chunks, rows), block(256);
+  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, (uint64_t*)workspace); };
+  if (dtype == YOCO_F32) vecs == 1 ? go(&select_chunks_kernel<float, 1>) : vecs == 2 ? go(&select_chunks_kernel<float, 2>) : go(&select_chunks_kernel<float, 4>);
+  else vecs == 1 ? go(&select_chunks_kernel<bf16_t, 1>) : vecs == 2 ? go(&select_chunks_kernel<bf16_t, 2>) : go(&select_chunks_kernel<bf16_t, 4>);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(select_merge_kernel, dim3(a.B), block, 0, s, a, (const uint64_t*)workspace, chunks);
+  return hipGetLastError();
+}
+
+hipError_t launch_beam_reorder_rows(const ReorderRows& r, int n, int B, int W, const int32_t* parent, hipStream_t s) {
+  int64_t most = 1;
+  for (int i = 0; i < n; ++i) most = r.pieces[i] > most ? r.pieces[i] : most;
+  const int64_t blocks = (most + 255) / 256;
+  const dim3 grid((unsigned)(blocks < 4096 ? blocks : 4096), B, n);
+  by_beams(W, [&](auto wm) { hipLaunchKernelGGL(reorder_rows_kernel<decltype(wm)::value>, grid, dim3(256), 0, s, r, W, parent); });
+  return hipGetLastError();
+}
+
+hipError_t launch_beam_reorder_pages(const yoco_paged_cache& c, int32_t* table, const int32_t* home, int B, int W, int cols, const int32_t* parent, const int64_t* lens,
+                                     hipStream_t s) {
+  const int64_t pieces = (int64_t)c.Hkv * page_bytes(c.d, c.dtype) / 16, blocks = (pieces + 255) / 256;
+  by_beams(W, [&](auto wm) {
+    constexpr int WM = decltype(wm)::value;
+    hipLaunchKernelGGL(reorder_tail_kernel<WM>, dim3((unsigned)(blocks < 1024 ? blocks : 1024), B, 2), dim3(256), 0, s, c, table, home, W, cols, parent, lens);
+    hipLaunchKernelGGL(reorder_table_kernel<WM>, dim3((cols + 255) / 256, B), dim3(256), 0, s, table, home, W, cols, parent, lens);
+  });
+  return hipGetLastError();
+}
+
+}  // namespace yoco

@@ -16,6 +16,9 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <memory>
+#include <vector>
+
 #include "yoco.h"
 
 namespace {
@@ -24,7 +27,9 @@ PyObject* g_error = nullptr;             // YocoError
 
 #define YOCO_CALLS(X)                                                                                                       \
   X(yoco_last_error_string) X(yoco_swa_prefill) X(yoco_global_kv_write_scaled) X(yoco_cross_attn_prefill) X(yoco_cross_attn_prefill_workspace) X(yoco_cross_attn_decode) \
-  X(yoco_cross_attn_decode_noalloc) X(yoco_swa_cache_write) X(yoco_kv_cache_append) X(yoco_swa_decode) X(yoco_gret_prefill) X(yoco_gret_decode)
+  X(yoco_cross_attn_decode_noalloc) X(yoco_swa_cache_write) X(yoco_kv_cache_append) X(yoco_swa_decode) X(yoco_gret_prefill) X(yoco_gret_decode) \
+  X(yoco_paged_append) X(yoco_paged_read) X(yoco_paged_attn_workspace) X(yoco_paged_attn) X(yoco_beam_select_workspace) X(yoco_beam_select) \
+  X(yoco_beam_reorder_pages) X(yoco_beam_reorder_rows)
 #define X(name) decltype(&::name) p_##name = nullptr;
 YOCO_CALLS(X)
 #undef X
@@ -386,6 +391,209 @@ PyObject* gret_decode(PyObject* const* a) {
   return wrap(o, a[8]);
 }
 
+// ---- the cache in pages
+yoco_paged_cache pages(PyObject* o) {
+  void* p = PyLong_AsVoidPtr(o);
+  if (!p) {
+    if (!PyErr_Occurred()) PyErr_SetString(g_error, "null cache");
+    throw Failed();
+  }
+  return *(const yoco_paged_cache*)p;
+}
+struct Table {
+  int32_t* p;
+  int64_t B, cols;
+};
+Table table(PyObject* o, const char* name) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.scalar_type() != at::kInt || t.dim() != 2) fail("%s must be int32 [B,cols]", name);
+  return {(int32_t*)dev(t, name), t.size(0), t.size(1)};
+}
+const int64_t* longs(PyObject* o, const char* name, int64_t n) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.scalar_type() != at::kLong || t.dim() != 1 || t.size(0) != n) fail("%s must be int64 [%lld]", name, (long long)n);
+  return (const int64_t*)dev(t, name);
+}
+int small(int64_t x, const char* name) {
+  if (x < 0 || x > INT32_MAX) fail("%s %lld is out of range", name, (long long)x);
+  return (int)x;
+}
+// Where the rows [B,T,H,d] of a tensor begin, and how far they are apart: heads dense, rows evenly apart over B and T.
+struct Strided {
+  void* p;
+  int64_t stride;
+};
+Strided strided(const at::Tensor& t, const char* name) {
+  if (!t.is_cuda()) fail("%s must be a device tensor", name);
+  const int64_t B = t.size(0), T = t.size(1), H = t.size(2), d = t.size(3);
+  const bool dense = t.stride(3) == 1 && (H == 1 || t.stride(2) == d);
+  const int64_t stride = T > 1 ? t.stride(1) : B > 1 ? t.stride(0) : H * d;
+  if (!dense || (T > 1 && B > 1 && t.stride(0) != T * stride)) fail("%s must have dense heads and rows evenly apart", name);
+  return {t.data_ptr(), stride};
+}
+bool is_rows(const at::Tensor& t, int64_t B, int64_t T, int64_t H, int64_t d) { return t.dim() == 4 && t.size(0) == B && t.size(1) == T && t.size(2) == H && t.size(3) == d; }
+// The caller's workspace, or one of `need` bytes from torch's pool of the current stream, to which it goes back when the call is enqueued.
+Workspace scratch(PyObject* given, size_t need, const at::TensorOptions& on, at::Tensor& held) {
+  Workspace w = workspace(given);
+  if (none(given) && need) {
+    held = at::empty({(int64_t)need}, on.dtype(at::kByte));
+    w = {held.data_ptr(), need};
+  }
+  return w;
+}
+
+// cache, table, pos, k, v, rows, q, turns, neighbours, q_out
+PyObject* paged_append(PyObject* const* a) {
+  const yoco_paged_cache c = pages(a[0]);
+  const Table t = table(a[1], "table");
+  const at::Tensor &k = tensor(a[3], "k"), &v = tensor(a[4], "v");
+  if (k.dim() != 4 || !is_rows(k, t.B, k.size(1), c.Hkv, c.d) || v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type()) fail("k/v must be [B,T,Hkv,d] as the table and the cache are");
+  const int64_t T = k.size(1);
+  const int64_t *pos = longs(a[2], "pos", t.B), *rows = none(a[5]) ? nullptr : longs(a[5], "rows", t.B);
+  const int dt = dtype_of(k);
+  at::Tensor o;
+  Strided q = {nullptr, 0};
+  int64_t Hq = 0;
+  if (!none(a[6])) {
+    const at::Tensor& x = tensor(a[6], "q");
+    if (x.dim() != 4 || !is_rows(x, t.B, T, x.size(2), c.d) || x.scalar_type() != k.scalar_type()) fail("q must be [B,T,Hq,d] of the type of k");
+    Hq = x.size(2);
+    o = output(a[9], x);
+    if (T) q = strided(x, "q");
+  } else if (!none(a[9])) {
+    fail("q_out without q");
+  }
+  yoco_rotation r = {nullptr, 0, truth(a[8])};
+  if (!none(a[7])) {
+    const at::Tensor& x = tensor(a[7], "turns");
+    if (x.scalar_type() != at::kLong || x.dim() != 1) fail("turns must be int64 [dims / 2]");
+    r.turns = (const uint64_t*)dev(x, "turns");
+    r.dims = small(2 * x.size(0), "turns");
+  }
+  const Strided ks = T ? strided(k, "k") : Strided{nullptr, 0}, vs = T ? strided(v, "v") : Strided{nullptr, 0};
+  void* op = o.defined() && T ? dev(o, "q_out") : nullptr;
+  const int B = small(t.B, "B"), cols = small(t.cols, "cols");
+  call([&] {
+    return p_yoco_paged_append(&c, t.p, B, cols, pos, rows, T, ks.p, ks.stride, vs.p, vs.stride, q.p, q.stride, op, (int)Hq, r.turns ? &r : nullptr, dt, stream());
+  });
+  return o.defined() ? wrap(o, a[9]) : nothing();
+}
+
+// cache, table, pos, T, k, v
+PyObject* paged_read(PyObject* const* a) {
+  const yoco_paged_cache c = pages(a[0]);
+  const Table t = table(a[1], "table");
+  const int64_t* pos = longs(a[2], "pos", t.B);
+  const int64_t T = integer(a[3]);
+  const at::Tensor &k = tensor(a[4], "k"), &v = tensor(a[5], "v");
+  if (!is_rows(k, t.B, T, c.Hkv, c.d) || v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type()) fail("k/v must be [B,T,Hkv,d] as the table and the cache are");
+  void *kp = dev(k, "k"), *vp = dev(v, "v");
+  const int dt = dtype_of(k), B = small(t.B, "B"), cols = small(t.cols, "cols");
+  call([&] { return p_yoco_paged_read(&c, t.p, B, cols, pos, T, kp, vp, dt, stream()); });
+  return nothing();
+}
+
+// cache, table, q, lens, scale, workspace, out
+PyObject* paged_attn(PyObject* const* a) {
+  const yoco_paged_cache c = pages(a[0]);
+  const Table t = table(a[1], "table");
+  const at::Tensor& q = tensor(a[2], "q");
+  if (q.dim() != 4 || !is_rows(q, t.B, q.size(1), q.size(2), c.d) || q.scalar_type() != at::kBFloat16) fail("q must be bfloat16 [B,T,Hq,d] as the table and the cache are");
+  const int64_t* lens = longs(a[3], "lens", t.B);
+  const float scale = real(a[4]);
+  const at::Tensor o = output(a[6], q);
+  void *qp = dev(q, "q"), *op = dev(o, "o");
+  const int B = small(t.B, "B"), cols = small(t.cols, "cols"), T = small(q.size(1), "T"), Hq = small(q.size(2), "Hq");
+  size_t need = 0;
+  if (none(a[5])) call([&] { return p_yoco_paged_attn_workspace(&c, B, cols, T, Hq, &need); });
+  at::Tensor held;
+  const Workspace w = scratch(a[5], need, q.options(), held);
+  call([&] { return p_yoco_paged_attn(&c, t.p, B, cols, qp, op, lens, T, Hq, scale, w.p, w.bytes, stream()); });
+  return wrap(o, a[6]);
+}
+
+void* beams(PyObject* o, const char* name, at::ScalarType type, const char* type_name, int64_t B, int64_t W) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.scalar_type() != type || t.dim() != 2 || t.size(0) != B || t.size(1) != W) fail("%s must be %s [B,W]", name, type_name);
+  return dev(t, name);
+}
+
+// logits, scores, done, eos, workspace -> (parent, token, scores, done)
+PyObject* beam_select(PyObject* const* a) {
+  const at::Tensor& x = tensor(a[0], "logits");
+  if (x.dim() != 3) fail("logits must be [B,W,V]");
+  const int B = small(x.size(0), "B"), W = small(x.size(1), "W"), V = small(x.size(2), "V");
+  if (!x.is_cuda()) fail("logits must be a device tensor");
+  const int64_t stride = W > 1 ? x.stride(1) : B > 1 ? x.stride(0) : V;
+  if ((V > 1 && x.stride(2) != 1) || (W > 1 && B > 1 && x.stride(0) != W * stride)) fail("logits must have dense rows, evenly apart");
+  const int dt = dtype_of(x);
+  const float* scores = (const float*)beams(a[1], "scores", at::kFloat, "float32", B, W);
+  const uint8_t* done = none(a[2]) ? nullptr : (const uint8_t*)beams(a[2], "done", at::kBool, "bool", B, W);
+  const int64_t eos = integer(a[3]);
+  if (eos > INT32_MAX) fail("eos is out of range");
+  size_t need = 0;
+  call([&] { return p_yoco_beam_select_workspace(B, W, V, &need); });
+  at::Tensor held;
+  const Workspace w = scratch(a[4], need, x.options(), held);
+  const at::Tensor parent = at::empty({B, W}, x.options().dtype(at::kInt)), token = at::empty({B, W}, x.options().dtype(at::kInt));
+  const at::Tensor best = at::empty({B, W}, x.options().dtype(at::kFloat)), ended = at::empty({B, W}, x.options().dtype(at::kBool));
+  void *xp = x.data_ptr(), *pp = parent.data_ptr(), *tp = token.data_ptr(), *bp = best.data_ptr(), *ep = ended.data_ptr();
+  call([&] {
+    return p_yoco_beam_select(xp, stride, scores, done, eos < 0 ? -1 : (int)eos, B, W, V, dt, (int32_t*)pp, (int32_t*)tp, (float*)bp, (uint8_t*)ep, w.p, w.bytes, stream());
+  });
+  PyObject* const out[4] = {THPVariable_Wrap(parent), THPVariable_Wrap(token), THPVariable_Wrap(best), THPVariable_Wrap(ended)};
+  PyObject* tuple = PyTuple_New(4);
+  bool ok = tuple != nullptr;
+  for (PyObject* x : out) ok = ok && x;
+  for (int i = 0; i < 4; ++i) {
+    if (ok) PyTuple_SET_ITEM(tuple, i, out[i]);
+    else Py_XDECREF(out[i]);
+  }
+  if (!ok) {
+    Py_XDECREF(tuple);
+    return nullptr;
+  }
+  return tuple;
+}
+
+// cache, table, home, parent, lens
+PyObject* beam_reorder_pages(PyObject* const* a) {
+  const yoco_paged_cache c = pages(a[0]);
+  const Table t = table(a[1], "table"), h = table(a[2], "home");
+  if (h.B != t.B || h.cols != t.cols) fail("home must be as large as the table");
+  const at::Tensor& x = tensor(a[3], "parent");
+  if (x.dim() != 2 || x.numel() != t.B) fail("parent must be int32 [B,W] with a beam a row of the table");
+  const int B = small(x.size(0), "B"), W = small(x.size(1), "W"), cols = small(t.cols, "cols");
+  const int32_t* parent = (const int32_t*)beams(a[3], "parent", at::kInt, "int32", B, W);
+  const int64_t* lens = longs(a[4], "lens", t.B);
+  call([&] { return p_yoco_beam_reorder_pages(&c, t.p, h.p, B, W, cols, parent, lens, stream()); });
+  return nothing();
+}
+
+// a list of tensors [B * W, ...], parent
+PyObject* beam_reorder_rows(PyObject* const* a) {
+  const at::Tensor& x = tensor(a[1], "parent");
+  if (x.dim() != 2) fail("parent must be int32 [B,W]");
+  const int B = small(x.size(0), "B"), W = small(x.size(1), "W");
+  const int32_t* parent = (const int32_t*)beams(a[1], "parent", at::kInt, "int32", B, W);
+  PyObject* const list = PySequence_Fast(a[0], "states must be a sequence of tensors");
+  if (!list) throw Failed();
+  const auto drop = [](PyObject* o) { Py_DECREF(o); };
+  const std::unique_ptr<PyObject, decltype(drop)> held(list, drop);
+  std::vector<void*> mem;
+  std::vector<int64_t> bytes;
+  for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(list); ++i) {
+    const at::Tensor& t = tensor(PySequence_Fast_GET_ITEM(list, i), "a state");
+    if (!t.dim() || t.size(0) != (int64_t)B * W) fail("state %zd must have a row a beam", i);
+    if (!t.numel()) continue;
+    mem.push_back(dev(t, "a state"));
+    bytes.push_back((int64_t)(t.nbytes() / t.size(0)));
+  }
+  const int n = small((int64_t)mem.size(), "states");
+  call([&] { return p_yoco_beam_reorder_rows(mem.data(), bytes.data(), n, B, W, parent, stream()); });
+  return nothing();
+}
+
 // path of libyoco, the exception type
 PyObject* init(PyObject*, PyObject* args) {
   const char* path = nullptr;
@@ -415,6 +623,12 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          ENTRY(swa_decode, 8),
                          ENTRY(gret_prefill, 13),
                          ENTRY(gret_decode, 10),
+                         ENTRY(paged_append, 10),
+                         ENTRY(paged_read, 6),
+                         ENTRY(paged_attn, 7),
+                         ENTRY(beam_select, 5),
+                         ENTRY(beam_reorder_pages, 5),
+                         ENTRY(beam_reorder_rows, 2),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

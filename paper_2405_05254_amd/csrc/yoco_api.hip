@@ -9,6 +9,7 @@
 #include <chrono>
 #include <mutex>
 
+#include "paged.h"
 #include "yoco_common.h"
 
 int yoco::compute_units() {
@@ -339,6 +340,45 @@ int scratch_of_current_device(void** out) {
     g_scratch_ptr[dev] = p;
   }
   *out = g_scratch_ptr[dev];
+  return YOCO_OK;
+}
+
+int check_pages(const yoco_paged_cache* c) {
+  if (!c) return fail(YOCO_ERR_INVALID_ARG, "cache descriptor is null");
+  if (!c->k || !c->v) return fail(YOCO_ERR_INVALID_ARG, "cache pages are null");
+  if (c->n_pages <= 0 || c->Hkv <= 0) return fail(YOCO_ERR_INVALID_ARG, "cache has a non-positive size");
+  if (c->dtype != YOCO_BF16 && c->dtype != YOCO_INT4) return fail(YOCO_ERR_UNSUPPORTED, "a cache in pages is bf16 or 4-bit, not dtype %d", c->dtype);
+  if (c->d != 64 && c->d != 128) return fail(YOCO_ERR_UNSUPPORTED, "a cache in pages needs head_dim 64 or 128, not %d", c->d);
+  if (c->Hkv > 65535) return fail(YOCO_ERR_UNSUPPORTED, "Hkv %d exceeds the grid limit", c->Hkv);
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(YOCO_ERR_ALIGNMENT, "cache pages are not 16-byte aligned");
+  return YOCO_OK;
+}
+int check_table(const int32_t* table, int B, int cols) {
+  if (!table) return fail(YOCO_ERR_INVALID_ARG, "table is null");
+  if (B <= 0 || cols <= 0) return fail(YOCO_ERR_INVALID_ARG, "non-positive B or cols");
+  if (B > 65535) return fail(YOCO_ERR_UNSUPPORTED, "B %d exceeds the grid limit", B);
+  if (cols > 1 << 24) return fail(YOCO_ERR_UNSUPPORTED, "cols %d exceeds 2^24", cols);
+  if (((uintptr_t)table) & 3u) return fail(YOCO_ERR_ALIGNMENT, "table is not 4-byte aligned");
+  return YOCO_OK;
+}
+int check_beams(int B, int W) {
+  if (B <= 0 || W <= 0) return fail(YOCO_ERR_INVALID_ARG, "non-positive B or W");
+  if (W > YOCO_MAX_BEAMS) return fail(YOCO_ERR_UNSUPPORTED, "%d beams, at most %d", W, YOCO_MAX_BEAMS);
+  if ((int64_t)B * W > 65535) return fail(YOCO_ERR_UNSUPPORTED, "%d requests of %d beams exceed the grid limit", B, W);
+  return YOCO_OK;
+}
+// Row r of a strided tensor begins 16-byte aligned: base and stride are.
+int check_strided(const void* p, int64_t stride, int64_t width, const char* name) {
+  if (!aligned16(p)) return fail(YOCO_ERR_ALIGNMENT, "%s is not 16-byte aligned", name);
+  if (stride < width) return fail(YOCO_ERR_INVALID_ARG, "rows of %s overlap: stride %lld, width %lld", name, (long long)stride, (long long)width);
+  if (stride % 8) return fail(YOCO_ERR_ALIGNMENT, "the row stride of %s is not a multiple of 8", name);
+  return YOCO_OK;
+}
+int check_attn_shape(int B, int cols, int T, int Hq, int Hkv) {
+  if (B <= 0 || cols <= 0 || T < 0) return fail(YOCO_ERR_INVALID_ARG, "non-positive B or cols, or negative T");
+  int rc = check_heads(Hq, Hkv);
+  if (rc) return rc;
+  if ((int64_t)T * Hq > 1 << 24) return fail(YOCO_ERR_UNSUPPORTED, "%d rows of %d heads are too many for one call", T, Hq);
   return YOCO_OK;
 }
 
@@ -808,6 +848,166 @@ int yoco_glu_rows(const void* gu, void* h, int64_t rows, int ffn, void* stream) 
   if (ffn % 8 || !aligned16(gu) || !aligned16(h)) return fail(YOCO_ERR_ALIGNMENT, "pointer not 16-byte aligned or ffn not a multiple of 8");
   if (rows == 0) return YOCO_OK;
   return hip_result(yoco::launch_glu_rows(gu, h, rows, ffn, (hipStream_t)stream), "glu_rows");
+}
+
+int yoco_paged_cache_bytes(int n_pages, int Hkv, int d, int dtype, size_t* bytes) {
+  if (!bytes) return fail(YOCO_ERR_INVALID_ARG, "bytes is null");
+  if (n_pages <= 0 || Hkv <= 0) return fail(YOCO_ERR_INVALID_ARG, "non-positive size");
+  if (dtype != YOCO_BF16 && dtype != YOCO_INT4) return fail(YOCO_ERR_UNSUPPORTED, "a cache in pages is bf16 or 4-bit, not dtype %d", dtype);
+  if (d != 64 && d != 128) return fail(YOCO_ERR_UNSUPPORTED, "a cache in pages needs head_dim 64 or 128, not %d", d);
+  *bytes = (size_t)2 * n_pages * Hkv * yoco::page_bytes(d, dtype);
+  return YOCO_OK;
+}
+
+int yoco_paged_cache_init(void* mem, size_t bytes, int n_pages, int Hkv, int d, int dtype, yoco_paged_cache* out) {
+  if (!out) return fail(YOCO_ERR_INVALID_ARG, "out is null");
+  if (!mem) return fail(YOCO_ERR_INVALID_ARG, "mem is null");
+  size_t need = 0;
+  int rc = yoco_paged_cache_bytes(n_pages, Hkv, d, dtype, &need);
+  if (rc) return rc;
+  if (bytes < need) return fail(YOCO_ERR_WORKSPACE, "cache memory %zu < %zu bytes", bytes, need);
+  if (((uintptr_t)mem) & 255u) return fail(YOCO_ERR_ALIGNMENT, "cache memory is not 256-byte aligned");
+  *out = {mem, (char*)mem + need / 2, n_pages, Hkv, d, dtype};
+  return YOCO_OK;
+}
+
+int yoco_paged_append(const yoco_paged_cache* c, const int32_t* table, int B, int cols, const int64_t* pos, const int64_t* rows, int64_t T, const void* k,
+                      int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int Hq, const yoco_rotation* rotation,
+                      int src_dtype, void* stream) {
+  int rc = check_pages(c);
+  if (rc) return rc;
+  rc = check_table(table, B, cols);
+  if (rc) return rc;
+  if (T < 0) return fail(YOCO_ERR_INVALID_ARG, "negative row count");
+  if (!dtype_ok(src_dtype)) return fail(YOCO_ERR_UNSUPPORTED, "source dtype %d", src_dtype);
+  if (rotation) {
+    if (rotation->dims <= 0 || rotation->dims > c->d || rotation->dims % 16)
+      return fail(YOCO_ERR_INVALID_ARG, "rotated dimensions %d are not a multiple of 16 up to %d", rotation->dims, c->d);
+    if (!rotation->turns) return fail(YOCO_ERR_INVALID_ARG, "turns is null");
+    if (((uintptr_t)rotation->turns) & 7u) return fail(YOCO_ERR_ALIGNMENT, "turns is not 8-byte aligned");
+  }
+  if (q && Hq <= 0) return fail(YOCO_ERR_INVALID_ARG, "non-positive head count");
+  if (q && Hq > 65535) return fail(YOCO_ERR_UNSUPPORTED, "Hq %d exceeds the grid limit", Hq);
+  if (T == 0) return YOCO_OK;
+  if ((int64_t)B * T > INT32_MAX || T > INT32_MAX) return fail(YOCO_ERR_UNSUPPORTED, "too many rows for one call");
+  if (!k || !v || !pos || (q && !q_out)) return fail(YOCO_ERR_INVALID_ARG, "null pointer");
+  if ((rc = check_strided(k, k_stride, (int64_t)c->Hkv * c->d, "k"))) return rc;
+  if ((rc = check_strided(v, v_stride, (int64_t)c->Hkv * c->d, "v"))) return rc;
+  if (q && (rc = check_strided(q, q_stride, (int64_t)Hq * c->d, "q"))) return rc;
+  if (q && !aligned16(q_out)) return fail(YOCO_ERR_ALIGNMENT, "q_out is not 16-byte aligned");
+  if (q && q_out == q && q_stride != (int64_t)Hq * c->d) return fail(YOCO_ERR_INVALID_ARG, "q_out may be q only where q is dense");
+  if ((((uintptr_t)pos) | ((uintptr_t)rows)) & 7u) return fail(YOCO_ERR_ALIGNMENT, "pos or rows is not 8-byte aligned");
+  const yoco::AppendView a = {*c, table, B, cols, pos, rows, T, k, v, q, q_out, k_stride, v_stride, q_stride, q ? Hq : 0,
+                              rotation ? rotation->turns : nullptr, rotation ? rotation->dims : 0, rotation ? rotation->neighbours != 0 : 0};
+  return hip_result(yoco::launch_paged_append(a, src_dtype, (hipStream_t)stream), "paged_append");
+}
+
+int yoco_paged_read(const yoco_paged_cache* c, const int32_t* table, int B, int cols, const int64_t* pos, int64_t T, void* k, void* v, int dst_dtype, void* stream) {
+  int rc = check_pages(c);
+  if (rc) return rc;
+  rc = check_table(table, B, cols);
+  if (rc) return rc;
+  if (T < 0) return fail(YOCO_ERR_INVALID_ARG, "negative row count");
+  if (!dtype_ok(dst_dtype)) return fail(YOCO_ERR_UNSUPPORTED, "destination dtype %d", dst_dtype);
+  if (T == 0) return YOCO_OK;
+  if (T > INT32_MAX || (int64_t)B * T > INT32_MAX || (int64_t)B * T * c->Hkv > INT32_MAX) return fail(YOCO_ERR_UNSUPPORTED, "too many rows for one call");
+  if (!k || !v || !pos) return fail(YOCO_ERR_INVALID_ARG, "null pointer");
+  if (!aligned16(k) || !aligned16(v)) return fail(YOCO_ERR_ALIGNMENT, "row pointer not 16-byte aligned");
+  if (((uintptr_t)pos) & 7u) return fail(YOCO_ERR_ALIGNMENT, "pos is not 8-byte aligned");
+  return hip_result(yoco::launch_paged_read(*c, table, B, cols, pos, T, k, v, dst_dtype, (hipStream_t)stream), "paged_read");
+}
+
+int yoco_paged_attn_workspace(const yoco_paged_cache* c, int B, int cols, int T, int Hq, size_t* bytes) {
+  if (!c || !bytes) return fail(YOCO_ERR_INVALID_ARG, "null argument");
+  if (c->Hkv <= 0 || (c->d != 64 && c->d != 128)) return fail(YOCO_ERR_INVALID_ARG, "cache has a size without kernels");
+  int rc = check_attn_shape(B, cols, T, Hq, c->Hkv);
+  if (rc) return rc;
+  const yoco::PagedAttnView a = {*c, nullptr, B, cols, nullptr, nullptr, nullptr, T, Hq, 0.f};
+  *bytes = T == 0 ? 0 : yoco::paged_attn_workspace(a);
+  return YOCO_OK;
+}
+
+int yoco_paged_attn(const yoco_paged_cache* c, const int32_t* table, int B, int cols, const void* q, void* o, const int64_t* lens, int T, int Hq, float scale,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_pages(c);
+  if (rc) return rc;
+  rc = check_table(table, B, cols);
+  if (rc) return rc;
+  rc = check_attn_shape(B, cols, T, Hq, c->Hkv);
+  if (rc || T == 0) return rc;
+  if (!q || !o || !lens) return fail(YOCO_ERR_INVALID_ARG, "null pointer");
+  if (!aligned16(q) || !aligned16(o) || !aligned16(workspace)) return fail(YOCO_ERR_ALIGNMENT, "pointer not 16-byte aligned");
+  if (((uintptr_t)lens) & 7u) return fail(YOCO_ERR_ALIGNMENT, "lens is not 8-byte aligned");
+  const yoco::PagedAttnView a = {*c, table, B, cols, q, o, lens, T, Hq, scale};
+  const size_t need = yoco::paged_attn_workspace(a);
+  if (need && (!workspace || workspace_bytes < need)) return fail(YOCO_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace ? workspace_bytes : (size_t)0, need);
+  return hip_result(yoco::launch_paged_attn(a, workspace, next_tag(), (hipStream_t)stream), "paged_attn");
+}
+
+int yoco_beam_select_workspace(int B, int W, int V, size_t* bytes) {
+  if (!bytes) return fail(YOCO_ERR_INVALID_ARG, "bytes is null");
+  int rc = check_beams(B, W);
+  if (rc) return rc;
+  if (V <= 0) return fail(YOCO_ERR_INVALID_ARG, "non-positive V");
+  if (V > 524288) return fail(YOCO_ERR_UNSUPPORTED, "a vocabulary of %d, at most 524288", V);
+  *bytes = yoco::beam_select_workspace(B, W, V);
+  return YOCO_OK;
+}
+
+int yoco_beam_select(const void* logits, int64_t stride, const float* scores, const uint8_t* done, int eos, int B, int W, int V, int dtype, int32_t* parent,
+                     int32_t* token, float* scores_out, uint8_t* done_out, void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  int rc = yoco_beam_select_workspace(B, W, V, &need);
+  if (rc) return rc;
+  if (!dtype_ok(dtype)) return fail(YOCO_ERR_UNSUPPORTED, "dtype %d", dtype);
+  if (!logits || !scores || !parent || !token || !scores_out || !workspace) return fail(YOCO_ERR_INVALID_ARG, "null pointer");
+  if (stride < V) return fail(YOCO_ERR_INVALID_ARG, "rows of logits overlap: stride %lld, %d words", (long long)stride, V);
+  if (stride > INT64_MAX / ((int64_t)B * W) / 8) return fail(YOCO_ERR_INVALID_ARG, "the row stride of logits is out of range");
+  if (done && eos >= V) return fail(YOCO_ERR_INVALID_ARG, "eos %d is no word of %d", eos, V);
+  if (!aligned16(logits) || !aligned16(workspace)) return fail(YOCO_ERR_ALIGNMENT, "pointer not 16-byte aligned");
+  if ((((uintptr_t)scores) | ((uintptr_t)parent) | ((uintptr_t)token) | ((uintptr_t)scores_out)) & 3u) return fail(YOCO_ERR_ALIGNMENT, "pointer not 4-byte aligned");
+  if (workspace_bytes < need) return fail(YOCO_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, need);
+  const yoco::SelectView a = {logits, stride, scores, done, eos, B, W, V, parent, token, scores_out, done_out};
+  return hip_result(yoco::launch_beam_select(a, dtype, workspace, (hipStream_t)stream), "beam_select");
+}
+
+int yoco_beam_reorder_pages(const yoco_paged_cache* c, int32_t* table, const int32_t* home, int B, int W, int cols, const int32_t* parent, const int64_t* lens,
+                            void* stream) {
+  int rc = check_pages(c);
+  if (rc) return rc;
+  rc = check_beams(B, W);
+  if (rc) return rc;
+  rc = check_table(table, B * W, cols);
+  if (rc) return rc;
+  if (!home || !parent || !lens) return fail(YOCO_ERR_INVALID_ARG, "null pointer");
+  if (home == table) return fail(YOCO_ERR_INVALID_ARG, "home and table are the same");
+  if ((((uintptr_t)home) | ((uintptr_t)parent)) & 3u) return fail(YOCO_ERR_ALIGNMENT, "pointer not 4-byte aligned");
+  if (((uintptr_t)lens) & 7u) return fail(YOCO_ERR_ALIGNMENT, "lens is not 8-byte aligned");
+  return hip_result(yoco::launch_beam_reorder_pages(*c, table, home, B, W, cols, parent, lens, (hipStream_t)stream), "beam_reorder_pages");
+}
+
+int yoco_beam_reorder_rows(void* const* mem, const int64_t* row_bytes, int n, int B, int W, const int32_t* parent, void* stream) {
+  int rc = check_beams(B, W);
+  if (rc) return rc;
+  if (n < 0) return fail(YOCO_ERR_INVALID_ARG, "negative buffer count");
+  if (n == 0) return YOCO_OK;
+  if (!mem || !row_bytes || !parent) return fail(YOCO_ERR_INVALID_ARG, "null pointer");
+  if (((uintptr_t)parent) & 3u) return fail(YOCO_ERR_ALIGNMENT, "parent is not 4-byte aligned");
+  for (int i = 0; i < n; ++i) {
+    if (!mem[i] || row_bytes[i] <= 0) return fail(YOCO_ERR_INVALID_ARG, "buffer %d is null or has empty rows", i);
+    if (!aligned16(mem[i]) || row_bytes[i] % 16) return fail(YOCO_ERR_ALIGNMENT, "buffer %d or its rows are not multiples of 16 bytes", i);
+  }
+  for (int i = 0; i < n; i += yoco::kReorderMost) {
+    yoco::ReorderRows r = {};
+    const int now = n - i < yoco::kReorderMost ? n - i : yoco::kReorderMost;
+    for (int j = 0; j < now; ++j) {
+      r.mem[j] = mem[i + j];
+      r.pieces[j] = row_bytes[i + j] / 16;
+    }
+    rc = hip_result(yoco::launch_beam_reorder_rows(r, now, B, W, parent, (hipStream_t)stream), "beam_reorder_rows");
+    if (rc) return rc;
+  }
+  return YOCO_OK;
 }
 
 int yoco_ceiling_mfma(const void* seed, void* sink, int iters, int workgroups, void* stream) {
