@@ -1,95 +1,603 @@
-// Attention over a cache in pages: o = softmax(scale q.k) v for the last T rows of every sequence, causal, d 64 or 128.
-#include "lanes.h"
+// Attention over a cache in pages: o = softmax(scale q.k) v for the last T rows of every sequence, causal, d 64 or 128, bf16 or
+// 4-bit pages. HBM-bound: every page is read once for all query heads of its KV head and up to 16 / G rows of the query.
+//
+// Work. The pages of all sequences and KV heads (and, of more than 16 columns = rows x heads of a KV head, column tiles) in a row
+// are cut into as many equal ranges as there are workgroups, so that ragged lengths end together. A range may hold the
+// end of one (sequence, head), whole ones, and the beginning of another; what is not whole goes to the workspace and is
+// merged by whoever finds all of it published (decode_tail.h says how that works without waiting or clearing).
+//
+// A workgroup's four wavefronts take turns at the pages. Both products are 16x16x32 matrix instructions whose operands are what a
+// page holds: S[key][column] = K q, then O[dim][column] += V^T P with the scores of a lane as they are, because the V plane
+// keeps the rows of a lane together.
+//
+// 4 bits. A dword of codes becomes four operand registers by an AND, a shift and two more of each: four bits under a mask are the
+// denormal fp16 code * 2^-24 or, one nibble up, code * 2^-20, which the matrix cores take exactly; the powers of two are put right in
+// the query (K) and the sums (V). Scales and minima act on sums: a score is
+//   sum_h scale_h (q_h . code_h) + min_h sum(q_h),   an output  sum_keys (p scale_h) code + sum_keys p min_h   (h: 64 dimensions).
+// With up to 4 (8) columns, 4 (2) pages are scored at once: the query stands in 4 columns of the operand for each page and is
+// zero in the others, so that the accumulators collect a page in every four columns and the softmax costs as much as one page's.
+#include "decode_tail.h"
+#include "mfma_util.h"
 #include "paged.h"
 
 namespace yoco {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// One query row and head a workgroup; its wavefronts take turns at the pages, a lane a row for the scores and d / 64 dimensions for the sums.
-template <int D, bool CODED>
-__global__ void __launch_bounds__(256) attn_kernel(PagedAttnView a) {
-  constexpr int kOwn = D / 64;
-  __shared__ float qs[D], ps[4][64], os[4][D], ms[4], ls[4];
-  const int h = blockIdx.x % a.Hq, i = blockIdx.x / a.Hq, b = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t row = ((int64_t)b * a.T + i) * a.Hq + h, most = (int64_t)a.cols * kPageRows;
-  const int64_t len = a.lens[b] < 0 ? 0 : a.lens[b] > most ? most : a.lens[b], seen = len - a.T + 1 + i;
-  if ((int)threadIdx.x < D) qs[threadIdx.x] = bf16_to_f32(((const bf16_t*)a.q)[row * D + threadIdx.x]) * (a.scale * kLog2e);
-  __syncthreads();
-  const int head = h / (a.Hq / a.c.Hkv);
-  float m = -INFINITY, l = 0.f, o[kOwn] = {};
-  for (int64_t p = wave; p * kPageRows < seen; p += 4) {
-    const int page = a.table[(int64_t)b * a.cols + p];
-    if (page < 0 || page >= a.c.n_pages) continue;
-    const int64_t at = ((int64_t)page * a.c.Hkv + head) * page_bytes(D, CODED ? YOCO_INT4 : YOCO_BF16);
-    const char *kp = (const char*)a.c.k + at, *vp = (const char*)a.c.v + at;
-    float s = 0.f;
-    for (int e = 0; e < D; ++e) {
-      float x;
-      if (CODED) {
-        const unsigned param = *(const unsigned*)(kp + param4_byte(lane, e, D));
-        const unsigned code = ((unsigned)(unsigned char)kp[k4_byte(lane, e, D)] >> (e % 2 * 4)) & 15u;
-        x = fmaf((float)code, __uint_as_float(param << 16), __uint_as_float(param & 0xffff0000u));
-      } else {
-        x = bf16_to_f32(((const bf16_t*)kp)[k16_at(lane, e, D)]);
-      }
-      s = fmaf(x, qs[e], s);
-    }
-    if (p * kPageRows + lane >= seen) s = -INFINITY;
-    const float m_new = fmaxf(m, over64<LaneMax>(s)), base = m_new == -INFINITY ? 0.f : m_new;
-    const float w = __builtin_amdgcn_exp2f(s - base), f = __builtin_amdgcn_exp2f(m - base);
-    m = m_new;
-    l = l * f + over64<LaneSum>(w);
-    ps[wave][lane] = w;
-    const int rows = seen - p * kPageRows < kPageRows ? (int)(seen - p * kPageRows) : kPageRows;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNegBig = -1.0e30f;      // "no row seen yet": finite, so m - m never makes NaN
+constexpr int kMinPages = 4;             // of a workgroup
+
+// What is cut into ranges. Everything fits 31 bits (the host sees to it).
+struct Ranges {
+  int heads;                             // KV heads x column tiles
+  int total, workgroups, each, more;     // `more` workgroups have each + 1 pages, the others each
+  __device__ __forceinline__ int begin(int w) const { return w * each + (w < more ? w : more); }
+  __device__ __forceinline__ int owner(int u) const {
+    const int big = more * (each + 1);
+    return u < big ? u / (each + 1) : more + (u - big) / each;
+  }
+};
+
+// A walk over the sequences, 64 at a time: a lane has one's pages and where they end.
+struct Walk {
+  const int64_t* lens;
+  int B, cols, first, before;            // the first of the 64, and the pages (times heads) before it
+  int pages, upto, len;                  // of this lane's sequence
+  __device__ __forceinline__ void load(int at) {
+    const int i = at + (int)(threadIdx.x & 63);
+    const int64_t most = (int64_t)cols * kPageRows, n = i < B ? lens[i] : 0;
+    first = at;
+    len = (int)(n < 0 ? 0 : n > most ? most : n);
+    pages = (len + kPageRows - 1) / kPageRows;
+    upto = lane_scan(pages, [](int a, int b) { return a + b; });
+  }
+};
+
+template <int D>
+struct Slot {                            // of a partial result: vectors, then (max, sum), then a tag for each wavefront
+  int columns;
+  __host__ __device__ size_t floats() const { return (size_t)columns * (D + 2) + 8; }
+  __device__ __forceinline__ int ml(int c) const { return columns * D + 2 * c; }
+  __device__ __forceinline__ int tag(int wave) const { return columns * (D + 2) + 2 * wave; }
+};
+
+struct Args {
+  yoco_paged_cache c;
+  const bf16_t* q;
+  bf16_t* o;
+  const int64_t* lens;
+  float* ws;
+  unsigned long long tag;
+  int B, cols, T, Hq, G, tiles;          // G: query heads of a KV head; tiles: of 16 columns
+  float scale;
+};
+
+// What a wavefront knows of its columns (lane n = lane % 16): one softmax state for each lane n.
+template <int D>
+struct State {
+  float m, l;
+  f32x4 o[D / 16];
+  float z[D / 64];                       // 4 bits: sum of p * minimum, this lane's rows
+  unsigned e;                            // 4 bits: exponent field of the largest scale so far; o is relative to 2^(e - 126)
+};
+
+__device__ __forceinline__ float exp2i(int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
+
+// ---- 4-bit pages
+__device__ __forceinline__ u32x4 nibbles_k(unsigned w) {      // dimensions (0,4) (1,5) (2,6) (3,7), the odd registers 16 times larger
+  const unsigned v = w >> 8;
+  return (u32x4){w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u};
+}
+__device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ u32x4 only(bool mine, u32x4 x) { return (u32x4){mine ? x[0] : 0u, mine ? x[1] : 0u, mine ? x[2] : 0u, mine ? x[3] : 0u}; }
+
+constexpr int kParamStride = 64 * 16 + 16;     // of a page's scales in LDS: the four pages of a read fall in distinct banks
+
+template <int D, int NP>
+struct Coded {
+  static constexpr int kGroups = D / 64, kSteps = D / 32, kLoads = D / 32;        // 16-byte loads of a plane's page
+  static constexpr int kPages = NP, kColumns = 16 / NP;
+  static constexpr int kLds = NP * kParamStride;
+  struct Page {
+    u32x4 x[kLoads];                     // codes of K, then of V
+    unsigned k[kGroups], v[kGroups];     // row `lane`'s scales and minima
+  };
+  struct Query {
+    u32x4 f[kSteps];
+    float sum[kGroups], c1, c2;          // of a group's numbers; what turns a sum of products into a score in log2 units
+  };
+
+  static __device__ __forceinline__ void load(Page& p, const char* at, int lane) {
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-      const int e = lane + 64 * j;
-      float sum = o[j] * f;
-      for (int r = 0; r < rows; ++r) {
-        float x;
-        if (CODED) {
-          const unsigned param = *(const unsigned*)(vp + param4_byte(r, e, D));
-          const unsigned code = ((unsigned)(unsigned char)vp[v4_byte(r, e)] >> (e / 16 % 2 * 4)) & 15u;
-          x = fmaf((float)code, __uint_as_float(param << 16), __uint_as_float(param & 0xffff0000u));
-        } else {
-          x = bf16_to_f32(((const bf16_t*)vp)[v16_at(r, e)]);
+    for (int u = 0; u < kLoads; ++u) p.x[u] = __builtin_nontemporal_load((const u32x4*)at + u * 64 + lane);
+  }
+  static __device__ __forceinline__ void load_params(Page& p, const char* k, const char* v, int lane) {
+#pragma unroll
+    for (int h = 0; h < kGroups; ++h) {
+      p.k[h] = __builtin_nontemporal_load((const unsigned*)(k + 32 * D) + lane * kGroups + h);
+      p.v[h] = __builtin_nontemporal_load((const unsigned*)(v + 32 * D) + lane * kGroups + h);
+    }
+  }
+  static __device__ __forceinline__ void begin(Page& p, const char* k, const char* v, int lane) {
+    load_params(p, k, v, lane);
+    load(p, k, lane);
+  }
+
+  // raw[t]: dimensions 32 t + 8 qg .. of this lane's column. Numbers are scaled by a power of two so that the largest is in [2^14, 2^15).
+  static __device__ __forceinline__ void prepare(Query& q, const u32x4 (&raw)[kSteps], float scale) {
+    unsigned most = 0;
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most = max(most, max(raw[t][i] & 0x7fffu, (raw[t][i] >> 16) & 0x7fffu));
+    most = max(most, (unsigned)__shfl_xor((int)most, 16));
+    most = max(most, (unsigned)__shfl_xor((int)most, 32));
+    const int up = 141 - (int)(most >> 7);
+#pragma unroll
+    for (int h = 0; h < kGroups; ++h) q.sum[h] = 0.f;
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __builtin_amdgcn_ldexpf(__uint_as_float(raw[t][i] << 16), up);
+        x[2 * i + 1] = __builtin_amdgcn_ldexpf(__uint_as_float(raw[t][i] & 0xffff0000u), up);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q.sum[t / 2] += x[i];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float f = p % 2 ? 0.0625f : 1.f;
+        q.f[t][p] = pack_f16(x[p] * f, x[p + 4] * f);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < kGroups; ++h) q.sum[h] = over_rows<LaneSum>(q.sum[h]) * 5.9604644775390625e-8f;      // 2^-24, as the sums of products have it
+    const int down = 24 - up, half = down / 2;
+    q.c1 = scale * kLog2e * exp2i(half);
+    q.c2 = most < 0x7f80u ? exp2i(down - half) : __uint_as_float(0x7fc00000u);                              // a query that is not finite
+  }
+
+  // NP pages: this lane's column has the page of its bank (lane % 16 / kColumns), of whose rows it sees nv; rows[j]: rows that page j has. v: pages
+  // of V; k2, v2: of the next step (MORE). A page's registers hold K, then V, then the next K: always four planes of pages on their way.
+  template <bool MORE>
+  static __device__ __forceinline__ void step(State<D>& st, const Query& q, Page (&x)[NP], int lane, int nv, const int (&rows)[NP], char* lds, const char* const (&v)[NP],
+                                              const char* const (&k2)[NP], const char* const (&v2)[NP]) {
+    const int qg = lane >> 4;
+    int bank = (lane & 15) / kColumns;
+    asm volatile("" : "+v"(bank));                                       // else the query is kept once for each bank: 64 registers
+    unsigned e_new = 0;
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      u32x4 par = {x[j].k[0], x[j].k[kGroups - 1], x[j].v[0], x[j].v[kGroups - 1]};
+      if (lane >= rows[j]) par = (u32x4){0u, 0u, 0u, 0u};        // whatever the memory held, NaN included
+      *(u32x4*)(lds + j * kParamStride + lane * 16) = par;
+      const unsigned e = (unsigned)lanes_max((int)((max(par[2] & 0x7f80u, par[3] & 0x7f80u)) >> 7));          // the page's largest scale
+      if (NP == 1 || bank == j) e_new = e;
+      if (MORE) load_params(x[j], k2[j], v2[j], lane);
+    }
+    e_new = max(e_new, st.e);
+    f32x4 acc[4][kGroups];
+#pragma unroll
+    for (int tau = 0; tau < 4; ++tau)
+#pragma unroll
+      for (int h = 0; h < kGroups; ++h) acc[tau][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      u32x4 f[kSteps];
+#pragma unroll
+      for (int t = 0; t < kSteps; ++t) f[t] = NP > 1 ? only(bank == j, q.f[t]) : q.f[t];
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) {
+          const int i = tau * kSteps + t;
+          acc[tau][t / 2] = mfma_f16(nibbles_k(x[j].x[i / 4][i % 4]), f[t], acc[tau][t / 2]);
         }
-        sum = fmaf(ps[wave][r], x, sum);
+        __builtin_amdgcn_sched_barrier(0);                               // few operands at a time, and the loads go where the codes were
       }
-      o[j] = sum;
+      load(x[j], v[j], lane);
+      __builtin_amdgcn_sched_barrier(0);
     }
-  }
+    // scores of rows 16 tau + 4 qg + i of the bank's page
+    float s[16], smax = -INFINITY;
+    const char* const mine = lds + bank * kParamStride + qg * 64;
 #pragma unroll
-  for (int j = 0; j < kOwn; ++j) os[wave][lane + 64 * j] = o[j];
-  if (lane == 0) {
-    ms[wave] = m;
-    ls[wave] = l;
-  }
-  __syncthreads();
-  if ((int)threadIdx.x < D) {
-    const float M = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])), base = M == -INFINITY ? 0.f : M;
-    float sum = 0.f, total = 0.f;
-    for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(ms[w] - base);
-      total = fmaf(f, ls[w], total);
-      sum = fmaf(f, os[w][threadIdx.x], sum);
+    for (int r = 0; r < 16; ++r) {
+      const int tau = r / 4, i = r % 4;
+      const u32x2 par = *(const u32x2*)(mine + (tau * 16 + i) * 16);
+      float a = 0.f;
+#pragma unroll
+      for (int h = 0; h < kGroups; ++h) {
+        a = fmaf(__uint_as_float(par[h] << 16), acc[tau][h][i], a);
+        a = fmaf(__uint_as_float(par[h] & 0xffff0000u), q.sum[h], a);
+      }
+      a = a * q.c1 * q.c2;
+      if (tau * 16 + qg * 4 + i >= nv) a = -INFINITY;
+      s[r] = a;
+      smax = fmaxf(smax, a);
     }
-    ((bf16_t*)a.o)[row * D + threadIdx.x] = f32_to_bf16(opaque_bits(total) ? sum / total : 0.f);
+    const float m_new = fmaxf(st.m, over_rows<LaneMax>(smax));           // the four lanes of a column hold 16 rows each
+    if (__builtin_amdgcn_ballot_w64(m_new != st.m || e_new != st.e)) {   // rare once the stream has met its large scores
+      const float alpha = __builtin_amdgcn_exp2f(st.m - m_new), beta = __builtin_amdgcn_exp2f(st.m - m_new + (float)((int)st.e - (int)e_new));
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) st.o[t] *= beta;
+#pragma unroll
+      for (int h = 0; h < kGroups; ++h) st.z[h] *= alpha;
+      st.l *= alpha;
+      st.m = m_new;
+      st.e = e_new;
+    }
+    const float down = exp2i(126 - (int)e_new);                          // scales below 1
+    u32x4 b[kGroups][2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      float w[kGroups][8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float p = __builtin_amdgcn_exp2f(s[half * 8 + r] - m_new), pd = p * down;
+        const u32x2 par = *(const u32x2*)(mine + ((half * 2 + r / 4) * 16 + r % 4) * 16 + 8);
+        st.l += p;
+#pragma unroll
+        for (int h = 0; h < kGroups; ++h) {
+          st.z[h] = fmaf(p, __uint_as_float(par[h] & 0xffff0000u), st.z[h]);
+          w[h][r] = __uint_as_float(par[h] << 16) * pd;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < kGroups; ++h)
+        b[h][half] = (u32x4){pack_f16(w[h][0], w[h][2]), pack_f16(w[h][1], w[h][3]), pack_f16(w[h][4], w[h][6]), pack_f16(w[h][5], w[h][7])};
+    }
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      u32x4 f[kGroups][2];
+#pragma unroll
+      for (int h = 0; h < kGroups; ++h)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) f[h][half] = NP > 1 ? only(bank == j, b[h][half]) : b[h][half];
+#pragma unroll
+      for (int t = 0; t < kLoads; ++t) {                                 // 32 dimensions: the low nibbles are 16 of them, the high ones the others
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const unsigned w0 = x[j].x[t][half * 2], w1 = x[j].x[t][half * 2 + 1], u0 = w0 >> 8, u1 = w1 >> 8;
+          st.o[2 * t] = mfma_f16((u32x4){w0 & 0x000f000fu, u0 & 0x000f000fu, w1 & 0x000f000fu, u1 & 0x000f000fu}, f[t / 2][half], st.o[2 * t]);
+          st.o[2 * t + 1] = mfma_f16((u32x4){w0 & 0x00f000f0u, u0 & 0x00f000f0u, w1 & 0x00f000f0u, u1 & 0x00f000f0u}, f[t / 2][half], st.o[2 * t + 1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (MORE) load(x[j], k2[j], lane);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // The state's vector as it is: dimensions 16 t + 4 qg + i.
+  static __device__ __forceinline__ void finish(State<D>& st) {
+    const float up = exp2i((int)st.e - 126 + 24);
+#pragma unroll
+    for (int h = 0; h < kGroups; ++h) {
+      const float z = over_rows<LaneSum>(st.z[h]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[h * 4 + t][i] = fmaf(st.o[h * 4 + t][i], t % 2 ? up * 0.0625f : up, z);
+    }
+  }
+};
+
+// ---- bf16 pages: softmax weights go in as a bf16 high part and a bf16 remainder (two products), which keeps 16 bits of them
+template <int D>
+struct Plain {
+  static constexpr int kSteps = D / 32, kLoads = D / 8, kPages = 1, kColumns = 16, kLds = 16;
+  struct Page {
+    u32x4 x[kLoads];                     // K, then V
+  };
+  struct Query {
+    u32x4 f[kSteps];
+    float scale;
+  };
+  static __device__ __forceinline__ u32x4 piece(const char* at, int u, int lane) { return __builtin_nontemporal_load((const u32x4*)at + u * 64 + lane); }
+  static __device__ __forceinline__ void begin(Page& p, const char* k, const char*, int lane) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) p.x[u] = piece(k, u, lane);
+  }
+  static __device__ __forceinline__ void prepare(Query& q, const u32x4 (&raw)[kSteps], float scale) {
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t) q.f[t] = raw[t];
+    q.scale = scale * kLog2e;
+  }
+  template <bool MORE>
+  static __device__ __forceinline__ void step(State<D>& st, const Query& q, Page (&x)[1], int lane, int nv, const int (&rows)[1], char*, const char* const (&v)[1], const char* const (&k2)[1],
+                                              const char* const (&)[1]) {
+    const int qg = lane >> 4;
+    float s[16];
+    float smax = -INFINITY;
+#pragma unroll
+    for (int tau = 0; tau < 4; ++tau) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < kSteps; ++t) {
+        acc = mfma_bf16(x[0].x[tau * kSteps + t], q.f[t], acc);
+        x[0].x[tau * kSteps + t] = piece(v[0], tau * kSteps + t, lane);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a = acc[i] * q.scale;
+        if (tau * 16 + qg * 4 + i >= nv) a = -INFINITY;
+        s[tau * 4 + i] = a;
+        smax = fmaxf(smax, a);
+      }
+    }
+    const float m_new = fmaxf(st.m, over_rows<LaneMax>(smax));
+    if (__builtin_amdgcn_ballot_w64(m_new != st.m)) {
+      const float alpha = __builtin_amdgcn_exp2f(st.m - m_new);
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) st.o[t] *= alpha;
+      st.l *= alpha;
+      st.m = m_new;
+    }
+    u32x4 hi[2], lo[2], there[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float a = __builtin_amdgcn_exp2f(s[half * 8 + 2 * p] - m_new), b = __builtin_amdgcn_exp2f(s[half * 8 + 2 * p + 1] - m_new);
+        st.l += a;
+        st.l += b;
+        const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
+        const float ra = a - __uint_as_float(ua & 0xffff0000u), rb = b - __uint_as_float(ub & 0xffff0000u);
+        hi[half][p] = (ua >> 16) | (ub & 0xffff0000u);
+        lo[half][p] = (__float_as_uint(ra) >> 16) | (__float_as_uint(rb) & 0xffff0000u);
+        const int r = (half * 2 + p / 2) * 16 + qg * 4 + p % 2 * 2;      // rows that the page does not have hold whatever the memory held
+        there[half][p] = (r < rows[0] ? 0x0000ffffu : 0u) | (r + 1 < rows[0] ? 0xffff0000u : 0u);
+      }
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        u32x4& w = x[0].x[t * 2 + half];
+        w &= there[half];
+        st.o[t] = mfma_bf16(w, hi[half], st.o[t]);
+        st.o[t] = mfma_bf16(w, lo[half], st.o[t]);
+        if (MORE) w = piece(k2[0], t * 2 + half, lane);
+      }
+  }
+  static __device__ __forceinline__ void finish(State<D>&) {}
+};
+
+__device__ __forceinline__ unsigned pair_bf16(float a, float b) { return (unsigned)f32_to_bf16(a) | ((unsigned)f32_to_bf16(b) << 16); }
+
+template <int D, typename Form>
+__global__ void __launch_bounds__(256, 2) attn_kernel(Args a, const int32_t* __restrict__ table) {
+  constexpr int NP = Form::kPages, NC = Form::kColumns, kRow = D + 4;
+  __shared__ __attribute__((aligned(16))) float red_o[4][16][kRow];
+  __shared__ float red_ml[4][16][2];
+  __shared__ __attribute__((aligned(16))) char params[4][Form::kLds];
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int n = lane & 15, qg = lane >> 4, bank = n / NC;
+  const size_t page_size = page_bytes(D, a.c.dtype);
+  const Slot<D> slot = {a.tiles > 1 ? NC : a.T * a.G};
+
+  // a sequence without rows has no pages: its outputs are zeros
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+    if (a.lens[b] <= 0)
+      for (int64_t i = threadIdx.x; i < (int64_t)a.T * a.Hq * (D / 2); i += 256) ((unsigned*)a.o)[(int64_t)b * a.T * a.Hq * (D / 2) + i] = 0;
+
+  Walk walk = {a.lens, a.B, a.cols};
+  Ranges r;
+  r.heads = a.c.Hkv * a.tiles;
+  int all = 0;
+  for (int at = 0; at < a.B; at += 64) {
+    walk.load(at);
+    all += last_lane(walk.upto);
+  }
+  r.total = all * r.heads;
+  r.workgroups = r.total / kMinPages < 1 ? 1 : r.total / kMinPages < (int)gridDim.x ? r.total / kMinPages : (int)gridDim.x;
+  r.each = r.total / r.workgroups;
+  r.more = r.total - r.each * r.workgroups;
+  const int me = blockIdx.x;
+  if (me >= r.workgroups || r.total == 0) return;
+  int u = r.begin(me);
+  const int end = r.begin(me + 1);
+  if (a.B > 64) walk.load(0);
+  walk.before = 0;
+
+  while (u < end) {
+    while (u >= walk.before + last_lane(walk.upto) * r.heads) {          // the next 64 sequences
+      walk.before += last_lane(walk.upto) * r.heads;
+      walk.load(walk.first + 64);
+    }
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(u < walk.before + walk.upto * r.heads));
+    const int P = __builtin_amdgcn_readlane(walk.pages, at), len = __builtin_amdgcn_readlane(walk.len, at);
+    const int b = walk.first + at, seq0 = walk.before + (__builtin_amdgcn_readlane(walk.upto, at) - P) * r.heads;
+    const int head = __builtin_amdgcn_readfirstlane((u - seq0) / P), seg0 = seq0 + head * P;
+    const int g = __builtin_amdgcn_readfirstlane(head / a.tiles), tile = head - g * a.tiles;
+    const int p0 = u - seg0, p1 = end - seg0 < P ? end - seg0 : P;
+    u = seg0 + p1;
+
+    // this lane's column: row ti and head of the query, and how many rows it sees
+    const int column = tile * 16 + n % NC, columns = a.T * a.G - tile * 16 < NC ? a.T * a.G - tile * 16 : NC;
+    const bool there = n % NC < columns;
+    const int ti = column / a.G, seen = there ? len - a.T + 1 + ti : len;
+    u32x4 raw[Form::kSteps] = {};
+    if (there) {
+      const bf16_t* const qp = a.q + (((int64_t)b * a.T + ti) * a.Hq + g * a.G + (column - ti * a.G)) * D + qg * 8;
+#pragma unroll
+      for (int t = 0; t < Form::kSteps; ++t) raw[t] = *(const u32x4*)(qp + t * 32);
+    }
+
+    const int32_t* const row = table + (int64_t)b * a.cols;
+    const char* const kp = (const char*)a.c.k + (size_t)g * page_size;
+    const char* const vp = (const char*)a.c.v + (size_t)g * page_size;
+    const size_t step_bytes = page_size * a.c.Hkv;
+    typename Form::Page x[NP];
+
+    State<D> st;
+    st.m = kNegBig;
+    st.l = 0.f;
+    st.e = 0;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) st.o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) st.z[h] = 0.f;
+
+    int first = p0 + wave;
+    const char *k[NP], *v[NP], *k2[NP], *v2[NP];
+    int rows[NP], rows2[NP];                                             // -1: no such page
+    auto find = [&](int from, const char* (&k)[NP], const char* (&v)[NP], int (&rows)[NP]) {
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        const int p = from + 4 * j, id = row[p < p1 ? p : p1 - 1], left = len - p * kPageRows;
+        const bool is = p < p1 && id >= 0 && id < a.c.n_pages;
+        rows[j] = is ? left < kPageRows ? left : kPageRows : -1;
+        k[j] = kp + (is ? id : 0) * step_bytes;
+        v[j] = vp + (is ? id : 0) * step_bytes;
+      }
+    };
+    if (first < p1) {
+      find(first, k, v, rows);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) Form::begin(x[j], k[j], v[j], lane);
+    }
+    typename Form::Query q;
+    Form::prepare(q, raw, a.scale);
+    if (first < p1) {
+      auto visible = [&] {                                               // rows of its bank's page that this lane's column sees
+        int nv = 0;
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+          if (NP == 1 || bank == j) nv = rows[j] < 0 ? 0 : seen - (first + 4 * j) * kPageRows;
+        return nv;
+      };
+      for (; first + 4 * NP < p1; first += 4 * NP) {
+        find(first + 4 * NP, k2, v2, rows2);
+        Form::template step<true>(st, q, x, lane, visible(), rows, params[wave], v, k2, v2);
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+          k[j] = k2[j];
+          v[j] = v2[j];
+          rows[j] = rows2[j];
+        }
+      }
+      Form::template step<false>(st, q, x, lane, visible(), rows, params[wave], v, k, v);
+    }
+    Form::finish(st);
+    const float l = over_rows<LaneSum>(st.l);
+    __syncthreads();                                                     // the merge of the segment before has been read
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) *(f32x4*)&red_o[wave][n][t * 16 + qg * 4] = st.o[t];
+    if (qg == 0) {
+      red_ml[wave][n][0] = st.m;
+      red_ml[wave][n][1] = l;
+    }
+    __syncthreads();
+
+    // A wavefront has every fourth column to itself: it merges the wavefronts' and banks' states, and publishes its part or, where it finds
+    // all parts published, merges those.
+    const bool whole = p0 == 0 && p1 == P;
+    const int part = 2 * me + (p0 == 0);
+    float* const mine = a.ws + (size_t)part * slot.floats();
+    const int e = lane * 2;
+    auto store = [&](int c, float o0, float o1, float sum) {             // no row seen: zeros
+      if (e >= D) return;
+      const int col = tile * 16 + c, t = col / a.G;
+      const float inv = opaque_bits(sum) ? 1.f / sum : 0.f;
+      *(unsigned*)(a.o + (((int64_t)b * a.T + t) * a.Hq + g * a.G + (col - t * a.G)) * D + e) = pair_bf16(o0 * inv, o1 * inv);
+    };
+    for (int c = wave; c < columns; c += 4) {
+      float M = kNegBig;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int j = 0; j < NP; ++j) M = fmaxf(M, red_ml[w][j * NC + c][0]);
+      float sum = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+          const float f = __builtin_amdgcn_exp2f(red_ml[w][j * NC + c][0] - M);
+          sum = fmaf(f, red_ml[w][j * NC + c][1], sum);
+          if (e < D) {
+            o0 = fmaf(f, red_o[w][j * NC + c][e], o0);
+            o1 = fmaf(f, red_o[w][j * NC + c][e + 1], o1);
+          }
+        }
+      if (whole) {
+        store(c, o0, o1, sum);
+      } else {
+        if (e < D) put_pair(mine + c * D + e, o0, o1);
+        if (lane == 0) put_pair(mine + slot.ml(c), M, sum);
+      }
+    }
+    if (whole || wave >= columns) continue;
+    wait_stores();
+    if (lane == 0) put_u64(mine + slot.tag(wave), a.tag);
+    wait_stores();
+    const int wa = r.owner(seg0), parts = r.owner(seg0 + P - 1) - wa + 1;
+    auto place = [&](int i) { return a.ws + (size_t)(2 * (wa + i) + (i == 0)) * slot.floats(); };          // the first part begins its segment
+    bool all_there = true;
+    for (int i = lane; i < parts; i += 64) all_there = all_there && get_u64(place(i) + slot.tag(wave)) == a.tag;
+    if (__builtin_amdgcn_ballot_w64(!all_there)) continue;
+    for (int c = wave; c < columns; c += 4) {
+      float M = kNegBig, sum = 0.f, o0 = 0.f, o1 = 0.f;
+      for (int i0 = 0; i0 < parts; i0 += 64) {                           // 64 parts at a time, a lane for the maximum and sum of each
+        const int i = i0 + lane < parts ? i0 + lane : parts - 1;
+        const unsigned long long ml = get_u64(place(i) + slot.ml(c));
+        const float m = i0 + lane < parts ? __uint_as_float((unsigned)ml) : kNegBig;
+        const float M2 = fmaxf(M, over64<LaneMax>(m)), old = __builtin_amdgcn_exp2f(M - M2);
+        const float f = i0 + lane < parts ? __builtin_amdgcn_exp2f(m - M2) : 0.f;
+        sum = sum * old + over64<LaneSum>(f * __uint_as_float((unsigned)(ml >> 32)));
+        o0 *= old;
+        o1 *= old;
+        M = M2;
+        const int here = parts - i0 < 64 ? parts - i0 : 64;
+        for (int k = 0; k < here; k += 16) {
+          unsigned long long y[16];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) y[v] = get_u64(place(i0 + (k + v < here ? k + v : here - 1)) + c * D + (e < D ? e : 0));
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const float fv = k + v < here ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k + v)) : 0.f;
+            if (k + v < here) {
+              o0 = fmaf(fv, __uint_as_float((unsigned)y[v]), o0);
+              o1 = fmaf(fv, __uint_as_float((unsigned)(y[v] >> 32)), o1);
+            }
+          }
+        }
+      }
+      store(c, o0, o1, sum);
+    }
+    for (int i = lane; i < parts; i += 64) put_u64(place(i) + slot.tag(wave), 0ull);     // a captured launch can be replayed
   }
 }
 
+int attn_workgroups() { return compute_units(); }
+
 }  // namespace
 
-size_t paged_attn_workspace(const PagedAttnView&) { return 0; }
+size_t paged_attn_workspace(const PagedAttnView& a) {
+  const int G = a.Hq / a.c.Hkv, columns = a.T * G < 16 ? a.T * G : 16;
+  const size_t floats = a.c.d == 128 ? Slot<128>{columns}.floats() : Slot<64>{columns}.floats();
+  return (size_t)2 * attn_workgroups() * floats * sizeof(float);
+}
 
-hipError_t launch_paged_attn(const PagedAttnView& a, void*, unsigned long long, hipStream_t s) {
-  const dim3 grid((unsigned)(a.T * a.Hq), (unsigned)a.B), block(256);
-  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
-  if (a.c.d == 128) a.c.dtype == YOCO_INT4 ? go(&attn_kernel<128, true>) : go(&attn_kernel<128, false>);
-  else a.c.dtype == YOCO_INT4 ? go(&attn_kernel<64, true>) : go(&attn_kernel<64, false>);
+hipError_t launch_paged_attn(const PagedAttnView& v, void* workspace, unsigned long long tag, hipStream_t s) {
+  const int G = v.Hq / v.c.Hkv, columns = v.T * G;
+  const Args a = {v.c, (const bf16_t*)v.q, (bf16_t*)v.o, v.lens, (float*)workspace, tag, v.B, v.cols, v.T, v.Hq, G, (columns + 15) / 16, v.scale};
+  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, dim3(attn_workgroups()), dim3(256), 0, s, a, v.table); };
+  if (v.c.dtype == YOCO_INT4) {
+    if (v.c.d == 128) columns <= 4 ? go(&attn_kernel<128, Coded<128, 4>>) : columns <= 8 ? go(&attn_kernel<128, Coded<128, 2>>) : go(&attn_kernel<128, Coded<128, 1>>);
+    else columns <= 4 ? go(&attn_kernel<64, Coded<64, 4>>) : columns <= 8 ? go(&attn_kernel<64, Coded<64, 2>>) : go(&attn_kernel<64, Coded<64, 1>>);
+  } else {
+    v.c.d == 128 ? go(&attn_kernel<128, Plain<128>>) : go(&attn_kernel<64, Plain<64>>);
+  }
   return hipGetLastError();
 }
 

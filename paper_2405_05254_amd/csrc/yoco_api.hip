@@ -378,7 +378,9 @@ int check_attn_shape(int B, int cols, int T, int Hq, int Hkv) {
   if (B <= 0 || cols <= 0 || T < 0) return fail(YOCO_ERR_INVALID_ARG, "non-positive B or cols, or negative T");
   int rc = check_heads(Hq, Hkv);
   if (rc) return rc;
-  if ((int64_t)T * Hq > 1 << 24) return fail(YOCO_ERR_UNSUPPORTED, "%d rows of %d heads are too many for one call", T, Hq);
+  // pages over all heads (and tiles of 16 rows and heads) are counted in 31 bits
+  if ((int64_t)T * Hq > 1 << 24 || (double)B * cols * Hkv * ((int64_t)T * (Hq / Hkv) / 16 + 1) > 2e9)
+    return fail(YOCO_ERR_UNSUPPORTED, "%d sequences of %d rows of %d heads over %d pages each are too many for one call", B, T, Hq, cols);
   return YOCO_OK;
 }
 
