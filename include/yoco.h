@@ -417,7 +417,7 @@ int yoco_glu_rows(const void* gu, void* h, int64_t rows, int ffn, void* stream);
 /*
  * ---- The global cache in pages ----
  * A pool of pages of YOCO_PAGE_ROWS rows, and for every sequence a row of a table that says which page holds its rows
- * 64 c .. 64 c + 63: table is int32 [B][cols] in device memory, so that a sequence holds up to 64 * cols rows. Sequences may
+ * 64 c .. 64 c + 63: table is int32 [B][cols] in device memory (cols up to 2^20), so that a sequence holds up to 64 * cols rows. Sequences may
  * share pages that neither of them writes any more (a common prompt). An entry outside [0, n_pages) stands for no page: its
  * rows are not written, and read as if they were not there. Who has which page is the caller's to decide.
  * Memory: the pages of K, then those of V, each [n_pages][Hkv][page of a head]. head_dim is 64 or 128. A page of a head, row r, dimension e:

@@ -28,33 +28,66 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegBig = -1.0e30f;      // "no row seen yet": finite, so m - m never makes NaN
-constexpr int kMinPages = 4;             // of a workgroup
+constexpr int kMinPages = 16;            // of a workgroup, where there are more
+constexpr int kManyPages = 32;
 
-// What is cut into ranges. Everything fits 31 bits (the host sees to it).
-struct Ranges {
-  int heads;                             // KV heads x column tiles
-  int total, workgroups, each, more;     // `more` workgroups have each + 1 pages, the others each
-  __device__ __forceinline__ int begin(int w) const { return w * each + (w < more ? w : more); }
-  __device__ __forceinline__ int owner(int u) const {
-    const int big = more * (each + 1);
-    return u < big ? u / (each + 1) : more + (u - big) / each;
-  }
+// What a workgroup takes: pages [p0, p1) of the P of a sequence, for a KV head (and column tile).
+struct Piece {
+  int b, head, len, p0, p1;
+  int part, parts, slot;                 // which of the pieces of this sequence and head, how many, and the first one's place in the workspace
+  bool any, many;                        // many: a wavefront has several steps of four pages
 };
 
-// A walk over the sequences, 64 at a time: a lane has one's pages and where they end.
-struct Walk {
-  const int64_t* lens;
-  int B, cols, first, before;            // the first of the 64, and the pages (times heads) before it
-  int pages, upto, len;                  // of this lane's sequence
-  __device__ __forceinline__ void load(int at) {
-    const int i = at + (int)(threadIdx.x & 63);
-    const int64_t most = (int64_t)cols * kPageRows, n = i < B ? lens[i] : 0;
-    first = at;
+__device__ __forceinline__ int up_to(int x, int by) { return (x + by - 1) / by * by; }
+
+// Every workgroup cuts the same lengths the same way, 64 sequences at a time, one a lane, and takes the piece of its number.
+__device__ __forceinline__ Piece piece_of(const int64_t* lens, int B, int cols, int heads, int units) {
+  const int lane = threadIdx.x & 63;
+  int len = 0, pages = 0;
+  auto look = [&](int at) {
+    const int64_t most = (int64_t)cols * kPageRows, n = at + lane < B ? lens[at + lane] : 0;
     len = (int)(n < 0 ? 0 : n > most ? most : n);
     pages = (len + kPageRows - 1) / kPageRows;
-    upto = lane_scan(pages, [](int a, int b) { return a + b; });
+  };
+  int total = 0;
+  for (int at = 0; at < B; at += 64) {
+    look(at);
+    total += lanes_sum(pages);
   }
-};
+  Piece x = {};
+  int share = total * heads / units + 1;
+  x.many = share >= kManyPages;
+  const int grain = x.many ? 16 : 4;
+  share = share < kMinPages ? kMinPages : up_to(share, grain);
+  int id = blockIdx.x, slots = 0;
+  for (int at = 0; at < B; at += 64) {
+    if (B > 64) look(at);
+    const int wanted = pages > share ? about_ceil_div(pages, share) : 1;
+    const int each = up_to(about_ceil_div(pages + 1, wanted), grain);    // + 1: above 0
+    const int n = pages > each ? about_ceil_div(pages, each) : 1;
+    const int count = at + lane < B ? n * heads : 0, split = n > 1 ? count : 0;
+    const auto plus = [](int a, int b) { return a + b; };
+    const int upto = lane_scan(count, plus), slots_upto = lane_scan(split, plus);
+    if (id < last_lane(upto)) {
+      const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(id < upto));
+      x.any = true;
+      x.b = at + i;
+      x.len = __builtin_amdgcn_readlane(len, i);
+      x.parts = __builtin_amdgcn_readlane(n, i);
+      const int mine = id - __builtin_amdgcn_readlane(upto - count, i), size = __builtin_amdgcn_readlane(each, i);
+      x.head = __builtin_amdgcn_readfirstlane(mine / x.parts);
+      x.part = mine - x.head * x.parts;
+      x.slot = slots + __builtin_amdgcn_readlane(slots_upto - split, i) + x.head * x.parts;
+      const int P = __builtin_amdgcn_readlane(pages, i);
+      x.p0 = x.part * size;
+      x.p1 = x.p0 + size < P ? x.p0 + size : P;
+      return x;
+    }
+    id -= last_lane(upto);
+    slots += last_lane(slots_upto);
+  }
+  return x;
+}
 
 template <int D>
 struct Slot {                            // of a partial result: vectors, then (max, sum), then a tag for each wavefront
@@ -71,7 +104,7 @@ struct Args {
   const int64_t* lens;
   float* ws;
   unsigned long long tag;
-  int B, cols, T, Hq, G, tiles;          // G: query heads of a KV head; tiles: of 16 columns
+  int B, cols, T, Hq, G, tiles, units;   // G: query heads of a KV head; tiles: of 16 columns; units: workgroups that the pages are shared out to
   float scale;
 };
 
@@ -106,8 +139,9 @@ struct Coded {
   static constexpr int kGroups = D / 64, kSteps = D / 32, kLoads = D / 32;        // 16-byte loads of a plane's page
   static constexpr int kPages = NP, kColumns = 16 / NP;
   static constexpr int kLds = NP * kParamStride;
+  static constexpr bool kApart = NP < 4; // K and V have registers of their own; else a page's are K's, then V's
   struct Page {
-    u32x4 x[kLoads];                     // codes of K, then of V
+    u32x4 x[kLoads], y[kApart ? kLoads : 0];
     unsigned k[kGroups], v[kGroups];     // row `lane`'s scales and minima
   };
   struct Query {
@@ -115,9 +149,13 @@ struct Coded {
     float sum[kGroups], c1, c2;          // of a group's numbers; what turns a sum of products into a score in log2 units
   };
 
-  static __device__ __forceinline__ void load(Page& p, const char* at, int lane) {
+  static __device__ __forceinline__ void load(u32x4 (&x)[kLoads], const char* at, int lane) {
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) p.x[u] = __builtin_nontemporal_load((const u32x4*)at + u * 64 + lane);
+    for (int u = 0; u < kLoads; ++u) x[u] = __builtin_nontemporal_load((const u32x4*)at + u * 64 + lane);
+  }
+  static __device__ __forceinline__ auto& codes_v(Page& p) {
+    if constexpr (kApart) return p.y;
+    else return p.x;
   }
   static __device__ __forceinline__ void load_params(Page& p, const char* k, const char* v, int lane) {
 #pragma unroll
@@ -127,8 +165,9 @@ struct Coded {
     }
   }
   static __device__ __forceinline__ void begin(Page& p, const char* k, const char* v, int lane) {
+    load(p.x, k, lane);
     load_params(p, k, v, lane);
-    load(p, k, lane);
+    if (kApart) load(codes_v(p), v, lane);
   }
 
   // raw[t]: dimensions 32 t + 8 qg .. of this lane's column. Numbers are scaled by a power of two so that the largest is in [2^14, 2^15).
@@ -167,9 +206,8 @@ struct Coded {
   }
 
   // NP pages: this lane's column has the page of its bank (lane % 16 / kColumns), of whose rows it sees nv; rows[j]: rows that page j has. v: pages
-  // of V; k2, v2: of the next step (MORE). A page's registers hold K, then V, then the next K: always four planes of pages on their way.
-  template <bool MORE>
-  static __device__ __forceinline__ void step(State<D>& st, const Query& q, Page (&x)[NP], int lane, int nv, const int (&rows)[NP], char* lds, const char* const (&v)[NP],
+  // of V; k2, v2: of the next step (more). Four planes of pages, two of one, are on their way at any time.
+    static __device__ __forceinline__ void step(State<D>& st, const Query& q, Page (&x)[NP], int lane, int nv, const int (&rows)[NP], char* lds, bool more, const char* const (&v)[NP],
                                               const char* const (&k2)[NP], const char* const (&v2)[NP]) {
     const int qg = lane >> 4;
     int bank = (lane & 15) / kColumns;
@@ -182,7 +220,7 @@ struct Coded {
       *(u32x4*)(lds + j * kParamStride + lane * 16) = par;
       const unsigned e = (unsigned)lanes_max((int)((max(par[2] & 0x7f80u, par[3] & 0x7f80u)) >> 7));          // the page's largest scale
       if (NP == 1 || bank == j) e_new = e;
-      if (MORE) load_params(x[j], k2[j], v2[j], lane);
+      if (more) load_params(x[j], k2[j], v2[j], lane);
     }
     e_new = max(e_new, st.e);
     f32x4 acc[4][kGroups];
@@ -204,7 +242,8 @@ struct Coded {
         }
         __builtin_amdgcn_sched_barrier(0);                               // few operands at a time, and the loads go where the codes were
       }
-      load(x[j], v[j], lane);
+      if constexpr (!kApart) load(x[j].x, v[j], lane);
+      else if (more) load(x[j].x, k2[j], lane);
       __builtin_amdgcn_sched_barrier(0);
     }
     // scores of rows 16 tau + 4 qg + i of the bank's page
@@ -267,13 +306,13 @@ struct Coded {
       for (int t = 0; t < kLoads; ++t) {                                 // 32 dimensions: the low nibbles are 16 of them, the high ones the others
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const unsigned w0 = x[j].x[t][half * 2], w1 = x[j].x[t][half * 2 + 1], u0 = w0 >> 8, u1 = w1 >> 8;
+          const unsigned w0 = codes_v(x[j])[t][half * 2], w1 = codes_v(x[j])[t][half * 2 + 1], u0 = w0 >> 8, u1 = w1 >> 8;
           st.o[2 * t] = mfma_f16((u32x4){w0 & 0x000f000fu, u0 & 0x000f000fu, w1 & 0x000f000fu, u1 & 0x000f000fu}, f[t / 2][half], st.o[2 * t]);
           st.o[2 * t + 1] = mfma_f16((u32x4){w0 & 0x00f000f0u, u0 & 0x00f000f0u, w1 & 0x00f000f0u, u1 & 0x00f000f0u}, f[t / 2][half], st.o[2 * t + 1]);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (MORE) load(x[j], k2[j], lane);
+      if (more) load(codes_v(x[j]), kApart ? v2[j] : k2[j], lane);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -313,8 +352,7 @@ struct Plain {
     for (int t = 0; t < kSteps; ++t) q.f[t] = raw[t];
     q.scale = scale * kLog2e;
   }
-  template <bool MORE>
-  static __device__ __forceinline__ void step(State<D>& st, const Query& q, Page (&x)[1], int lane, int nv, const int (&rows)[1], char*, const char* const (&v)[1], const char* const (&k2)[1],
+    static __device__ __forceinline__ void step(State<D>& st, const Query& q, Page (&x)[1], int lane, int nv, const int (&rows)[1], char*, bool more, const char* const (&v)[1], const char* const (&k2)[1],
                                               const char* const (&)[1]) {
     const int qg = lane >> 4;
     float s[16];
@@ -366,7 +404,7 @@ struct Plain {
         w &= there[half];
         st.o[t] = mfma_bf16(w, hi[half], st.o[t]);
         st.o[t] = mfma_bf16(w, lo[half], st.o[t]);
-        if (MORE) w = piece(k2[0], t * 2 + half, lane);
+        if (more) w = piece(k2[0], t * 2 + half, lane);
       }
   }
   static __device__ __forceinline__ void finish(State<D>&) {}
@@ -374,230 +412,209 @@ struct Plain {
 
 __device__ __forceinline__ unsigned pair_bf16(float a, float b) { return (unsigned)f32_to_bf16(a) | ((unsigned)f32_to_bf16(b) << 16); }
 
+template <int D>
+struct Lds {
+  float o[4][16][D + 4], ml[4][16][2];
+};
+
 template <int D, typename Form>
-__global__ void __launch_bounds__(256, 2) attn_kernel(Args a, const int32_t* __restrict__ table) {
-  constexpr int NP = Form::kPages, NC = Form::kColumns, kRow = D + 4;
-  __shared__ __attribute__((aligned(16))) float red_o[4][16][kRow];
-  __shared__ float red_ml[4][16][2];
-  __shared__ __attribute__((aligned(16))) char params[4][Form::kLds];
+__device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict__ table, const Piece& piece, Lds<D>& red, char* params) {
+  constexpr int NP = Form::kPages, NC = Form::kColumns;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int n = lane & 15, qg = lane >> 4, bank = n / NC;
   const size_t page_size = page_bytes(D, a.c.dtype);
-  const Slot<D> slot = {a.tiles > 1 ? NC : a.T * a.G};
+  const Slot<D> slot = {a.tiles > 1 ? 16 : a.T * a.G};
+  const int b = piece.b, len = piece.len, p1 = piece.p1;
+  const int g = a.tiles > 1 ? __builtin_amdgcn_readfirstlane(piece.head / a.tiles) : piece.head, tile = piece.head - g * a.tiles;
 
-  // a sequence without rows has no pages: its outputs are zeros
-  for (int b = blockIdx.x; b < a.B; b += gridDim.x)
-    if (a.lens[b] <= 0)
-      for (int64_t i = threadIdx.x; i < (int64_t)a.T * a.Hq * (D / 2); i += 256) ((unsigned*)a.o)[(int64_t)b * a.T * a.Hq * (D / 2) + i] = 0;
-
-  Walk walk = {a.lens, a.B, a.cols};
-  Ranges r;
-  r.heads = a.c.Hkv * a.tiles;
-  int all = 0;
-  for (int at = 0; at < a.B; at += 64) {
-    walk.load(at);
-    all += last_lane(walk.upto);
+  // this lane's column: row ti and head of the query, and how many rows it sees
+  const int column = tile * 16 + n % NC, columns = a.T * a.G - tile * 16 < NC ? a.T * a.G - tile * 16 : NC;
+  const bool there = n % NC < columns;
+  const int ti = a.T > 1 ? column / a.G : 0, seen = there ? len - a.T + 1 + ti : len;
+  u32x4 raw[Form::kSteps] = {};
+  if (there) {
+    const bf16_t* const qp = a.q + (((int64_t)b * a.T + ti) * a.Hq + g * a.G + (column - ti * a.G)) * D + qg * 8;
+#pragma unroll
+    for (int t = 0; t < Form::kSteps; ++t) raw[t] = *(const u32x4*)(qp + t * 32);
   }
-  r.total = all * r.heads;
-  r.workgroups = r.total / kMinPages < 1 ? 1 : r.total / kMinPages < (int)gridDim.x ? r.total / kMinPages : (int)gridDim.x;
-  r.each = r.total / r.workgroups;
-  r.more = r.total - r.each * r.workgroups;
-  const int me = blockIdx.x;
-  if (me >= r.workgroups || r.total == 0) return;
-  int u = r.begin(me);
-  const int end = r.begin(me + 1);
-  if (a.B > 64) walk.load(0);
-  walk.before = 0;
 
-  while (u < end) {
-    while (u >= walk.before + last_lane(walk.upto) * r.heads) {          // the next 64 sequences
-      walk.before += last_lane(walk.upto) * r.heads;
-      walk.load(walk.first + 64);
+  const int32_t* const row = table + (int64_t)b * a.cols;
+  const char* const kp = (const char*)a.c.k + (size_t)g * page_size;
+  const char* const vp = (const char*)a.c.v + (size_t)g * page_size;
+  const size_t step_bytes = page_size * a.c.Hkv;
+  typename Form::Page x[NP];
+  State<D> st;
+  st.m = kNegBig;
+  st.l = 0.f;
+  st.e = 0;
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) st.o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h) st.z[h] = 0.f;
+
+  int first = piece.p0 + wave;
+  const char *v[NP], *k2[NP], *v2[NP];
+  int rows[NP], rows2[NP];                                               // -1: no such page
+  auto find = [&](int from, const char* (&k)[NP], const char* (&v)[NP], int (&rows)[NP]) {
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      const int p = from + 4 * j, id = row[p < p1 ? p : p1 - 1], left = len - p * kPageRows;
+      const bool is = p < p1 && id >= 0 && id < a.c.n_pages;
+      rows[j] = is ? left < kPageRows ? left : kPageRows : -1;
+      k[j] = kp + (is ? id : 0) * step_bytes;
+      v[j] = vp + (is ? id : 0) * step_bytes;
     }
-    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(u < walk.before + walk.upto * r.heads));
-    const int P = __builtin_amdgcn_readlane(walk.pages, at), len = __builtin_amdgcn_readlane(walk.len, at);
-    const int b = walk.first + at, seq0 = walk.before + (__builtin_amdgcn_readlane(walk.upto, at) - P) * r.heads;
-    const int head = __builtin_amdgcn_readfirstlane((u - seq0) / P), seg0 = seq0 + head * P;
-    const int g = __builtin_amdgcn_readfirstlane(head / a.tiles), tile = head - g * a.tiles;
-    const int p0 = u - seg0, p1 = end - seg0 < P ? end - seg0 : P;
-    u = seg0 + p1;
-
-    // this lane's column: row ti and head of the query, and how many rows it sees
-    const int column = tile * 16 + n % NC, columns = a.T * a.G - tile * 16 < NC ? a.T * a.G - tile * 16 : NC;
-    const bool there = n % NC < columns;
-    const int ti = column / a.G, seen = there ? len - a.T + 1 + ti : len;
-    u32x4 raw[Form::kSteps] = {};
-    if (there) {
-      const bf16_t* const qp = a.q + (((int64_t)b * a.T + ti) * a.Hq + g * a.G + (column - ti * a.G)) * D + qg * 8;
+  };
+  if (first < p1) {
+    find(first, k2, v, rows);
 #pragma unroll
-      for (int t = 0; t < Form::kSteps; ++t) raw[t] = *(const u32x4*)(qp + t * 32);
-    }
-
-    const int32_t* const row = table + (int64_t)b * a.cols;
-    const char* const kp = (const char*)a.c.k + (size_t)g * page_size;
-    const char* const vp = (const char*)a.c.v + (size_t)g * page_size;
-    const size_t step_bytes = page_size * a.c.Hkv;
-    typename Form::Page x[NP];
-
-    State<D> st;
-    st.m = kNegBig;
-    st.l = 0.f;
-    st.e = 0;
-#pragma unroll
-    for (int t = 0; t < D / 16; ++t) st.o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int h = 0; h < D / 64; ++h) st.z[h] = 0.f;
-
-    int first = p0 + wave;
-    const char *k[NP], *v[NP], *k2[NP], *v2[NP];
-    int rows[NP], rows2[NP];                                             // -1: no such page
-    auto find = [&](int from, const char* (&k)[NP], const char* (&v)[NP], int (&rows)[NP]) {
-#pragma unroll
-      for (int j = 0; j < NP; ++j) {
-        const int p = from + 4 * j, id = row[p < p1 ? p : p1 - 1], left = len - p * kPageRows;
-        const bool is = p < p1 && id >= 0 && id < a.c.n_pages;
-        rows[j] = is ? left < kPageRows ? left : kPageRows : -1;
-        k[j] = kp + (is ? id : 0) * step_bytes;
-        v[j] = vp + (is ? id : 0) * step_bytes;
-      }
-    };
-    if (first < p1) {
-      find(first, k, v, rows);
-#pragma unroll
-      for (int j = 0; j < NP; ++j) Form::begin(x[j], k[j], v[j], lane);
-    }
+    for (int j = 0; j < NP; ++j) Form::begin(x[j], k2[j], v[j], lane);
     typename Form::Query q;
     Form::prepare(q, raw, a.scale);
-    if (first < p1) {
-      auto visible = [&] {                                               // rows of its bank's page that this lane's column sees
-        int nv = 0;
+    while (first < p1) {
+      int nv = 0;                                                        // rows of its bank's page that this lane's column sees
 #pragma unroll
-        for (int j = 0; j < NP; ++j)
-          if (NP == 1 || bank == j) nv = rows[j] < 0 ? 0 : seen - (first + 4 * j) * kPageRows;
-        return nv;
-      };
-      for (; first + 4 * NP < p1; first += 4 * NP) {
-        find(first + 4 * NP, k2, v2, rows2);
-        Form::template step<true>(st, q, x, lane, visible(), rows, params[wave], v, k2, v2);
+      for (int j = 0; j < NP; ++j)
+        if (NP == 1 || bank == j) nv = rows[j] < 0 ? 0 : seen - (first + 4 * j) * kPageRows;
+      first += 4 * NP;
+      const bool more = first < p1;
+      if (more) find(first, k2, v2, rows2);
+      Form::step(st, q, x, lane, nv, rows, params + wave * Form::kLds, more, v, k2, v2);
 #pragma unroll
-        for (int j = 0; j < NP; ++j) {
-          k[j] = k2[j];
-          v[j] = v2[j];
-          rows[j] = rows2[j];
-        }
-      }
-      Form::template step<false>(st, q, x, lane, visible(), rows, params[wave], v, k, v);
-    }
-    Form::finish(st);
-    const float l = over_rows<LaneSum>(st.l);
-    __syncthreads();                                                     // the merge of the segment before has been read
-#pragma unroll
-    for (int t = 0; t < D / 16; ++t) *(f32x4*)&red_o[wave][n][t * 16 + qg * 4] = st.o[t];
-    if (qg == 0) {
-      red_ml[wave][n][0] = st.m;
-      red_ml[wave][n][1] = l;
-    }
-    __syncthreads();
-
-    // A wavefront has every fourth column to itself: it merges the wavefronts' and banks' states, and publishes its part or, where it finds
-    // all parts published, merges those.
-    const bool whole = p0 == 0 && p1 == P;
-    const int part = 2 * me + (p0 == 0);
-    float* const mine = a.ws + (size_t)part * slot.floats();
-    const int e = lane * 2;
-    auto store = [&](int c, float o0, float o1, float sum) {             // no row seen: zeros
-      if (e >= D) return;
-      const int col = tile * 16 + c, t = col / a.G;
-      const float inv = opaque_bits(sum) ? 1.f / sum : 0.f;
-      *(unsigned*)(a.o + (((int64_t)b * a.T + t) * a.Hq + g * a.G + (col - t * a.G)) * D + e) = pair_bf16(o0 * inv, o1 * inv);
-    };
-    for (int c = wave; c < columns; c += 4) {
-      float M = kNegBig;
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-#pragma unroll
-        for (int j = 0; j < NP; ++j) M = fmaxf(M, red_ml[w][j * NC + c][0]);
-      float sum = 0.f, o0 = 0.f, o1 = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-#pragma unroll
-        for (int j = 0; j < NP; ++j) {
-          const float f = __builtin_amdgcn_exp2f(red_ml[w][j * NC + c][0] - M);
-          sum = fmaf(f, red_ml[w][j * NC + c][1], sum);
-          if (e < D) {
-            o0 = fmaf(f, red_o[w][j * NC + c][e], o0);
-            o1 = fmaf(f, red_o[w][j * NC + c][e + 1], o1);
-          }
-        }
-      if (whole) {
-        store(c, o0, o1, sum);
-      } else {
-        if (e < D) put_pair(mine + c * D + e, o0, o1);
-        if (lane == 0) put_pair(mine + slot.ml(c), M, sum);
+      for (int j = 0; j < NP; ++j) {
+        v[j] = v2[j];
+        rows[j] = rows2[j];
       }
     }
-    if (whole || wave >= columns) continue;
-    wait_stores();
-    if (lane == 0) put_u64(mine + slot.tag(wave), a.tag);
-    wait_stores();
-    const int wa = r.owner(seg0), parts = r.owner(seg0 + P - 1) - wa + 1;
-    auto place = [&](int i) { return a.ws + (size_t)(2 * (wa + i) + (i == 0)) * slot.floats(); };          // the first part begins its segment
-    bool all_there = true;
-    for (int i = lane; i < parts; i += 64) all_there = all_there && get_u64(place(i) + slot.tag(wave)) == a.tag;
-    if (__builtin_amdgcn_ballot_w64(!all_there)) continue;
-    for (int c = wave; c < columns; c += 4) {
-      float M = kNegBig, sum = 0.f, o0 = 0.f, o1 = 0.f;
-      for (int i0 = 0; i0 < parts; i0 += 64) {                           // 64 parts at a time, a lane for the maximum and sum of each
-        const int i = i0 + lane < parts ? i0 + lane : parts - 1;
-        const unsigned long long ml = get_u64(place(i) + slot.ml(c));
-        const float m = i0 + lane < parts ? __uint_as_float((unsigned)ml) : kNegBig;
-        const float M2 = fmaxf(M, over64<LaneMax>(m)), old = __builtin_amdgcn_exp2f(M - M2);
-        const float f = i0 + lane < parts ? __builtin_amdgcn_exp2f(m - M2) : 0.f;
-        sum = sum * old + over64<LaneSum>(f * __uint_as_float((unsigned)(ml >> 32)));
-        o0 *= old;
-        o1 *= old;
-        M = M2;
-        const int here = parts - i0 < 64 ? parts - i0 : 64;
-        for (int k = 0; k < here; k += 16) {
-          unsigned long long y[16];
-#pragma unroll
-          for (int v = 0; v < 16; ++v) y[v] = get_u64(place(i0 + (k + v < here ? k + v : here - 1)) + c * D + (e < D ? e : 0));
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const float fv = k + v < here ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k + v)) : 0.f;
-            if (k + v < here) {
-              o0 = fmaf(fv, __uint_as_float((unsigned)y[v]), o0);
-              o1 = fmaf(fv, __uint_as_float((unsigned)(y[v] >> 32)), o1);
-            }
-          }
-        }
-      }
-      store(c, o0, o1, sum);
-    }
-    for (int i = lane; i < parts; i += 64) put_u64(place(i) + slot.tag(wave), 0ull);     // a captured launch can be replayed
   }
+  Form::finish(st);
+  const float l = over_rows<LaneSum>(st.l);
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) *(f32x4*)&red.o[wave][n][t * 16 + qg * 4] = st.o[t];
+  if (qg == 0) {
+    red.ml[wave][n][0] = st.m;
+    red.ml[wave][n][1] = l;
+  }
+  __syncthreads();
+
+  // A wavefront has every fourth column to itself: it merges the wavefronts' and banks' states, and publishes its part or, where it finds
+  // all parts published, merges those.
+  const int parts = piece.parts, e = lane * 2;
+  auto place = [&](int i) { return a.ws + (size_t)(piece.slot + i) * slot.floats(); };
+  float* const mine = place(piece.part);
+  auto store = [&](int c, float o0, float o1, float sum) {               // no row seen: zeros
+    if (e >= D) return;
+    const int col = tile * 16 + c, t = a.T > 1 ? col / a.G : 0;
+    const float inv = opaque_bits(sum) ? 1.f / sum : 0.f;
+    *(unsigned*)(a.o + (((int64_t)b * a.T + t) * a.Hq + g * a.G + (col - t * a.G)) * D + e) = pair_bf16(o0 * inv, o1 * inv);
+  };
+  for (int c = wave; c < columns; c += 4) {
+    float M = kNegBig;
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int j = 0; j < NP; ++j) M = fmaxf(M, red.ml[w][j * NC + c][0]);
+    float sum = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        const float f = __builtin_amdgcn_exp2f(red.ml[w][j * NC + c][0] - M);
+        sum = fmaf(f, red.ml[w][j * NC + c][1], sum);
+        if (e < D) {
+          o0 = fmaf(f, red.o[w][j * NC + c][e], o0);
+          o1 = fmaf(f, red.o[w][j * NC + c][e + 1], o1);
+        }
+      }
+    if (parts == 1) {
+      store(c, o0, o1, sum);
+    } else {
+      if (e < D) put_pair(mine + c * D + e, o0, o1);
+      if (lane == 0) put_pair(mine + slot.ml(c), M, sum);
+    }
+  }
+  if (parts == 1 || wave >= columns) return;
+  wait_stores();
+  if (lane == 0) put_u64(mine + slot.tag(wave), a.tag);
+  wait_stores();
+  bool all_there = true;
+  for (int i = lane; i < parts; i += 64) all_there = all_there && get_u64(place(i) + slot.tag(wave)) == a.tag;
+  if (__builtin_amdgcn_ballot_w64(!all_there)) return;
+  for (int c = wave; c < columns; c += 4) {
+    float M = kNegBig, sum = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int i0 = 0; i0 < parts; i0 += 64) {                             // 64 parts at a time, a lane for the maximum and sum of each
+      const int i = i0 + lane < parts ? i0 + lane : parts - 1;
+      const unsigned long long ml = get_u64(place(i) + slot.ml(c));
+      const float m = i0 + lane < parts ? __uint_as_float((unsigned)ml) : kNegBig;
+      const float M2 = fmaxf(M, over64<LaneMax>(m)), old = __builtin_amdgcn_exp2f(M - M2);
+      const float f = i0 + lane < parts ? __builtin_amdgcn_exp2f(m - M2) : 0.f;
+      sum = sum * old + over64<LaneSum>(f * __uint_as_float((unsigned)(ml >> 32)));
+      o0 *= old;
+      o1 *= old;
+      M = M2;
+      const int here = parts - i0 < 64 ? parts - i0 : 64;
+      for (int k = 0; k < here; k += 16) {
+        unsigned long long y[16];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) y[v] = get_u64(place(i0 + (k + v < here ? k + v : here - 1)) + c * D + (e < D ? e : 0));
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          if (k + v >= here) break;
+          const float fv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k + v));
+          o0 = fmaf(fv, __uint_as_float((unsigned)y[v]), o0);
+          o1 = fmaf(fv, __uint_as_float((unsigned)(y[v] >> 32)), o1);
+        }
+      }
+    }
+    store(c, o0, o1, sum);
+  }
+  for (int i = lane; i < parts; i += 64) put_u64(place(i) + slot.tag(wave), 0ull);       // a captured launch can be replayed
 }
 
-int attn_workgroups() { return compute_units(); }
+// Long: the form where a wavefront has many pages.
+template <int D, typename Form, typename Long>
+__global__ void __launch_bounds__(256, 2) attn_kernel(Args a, const int32_t* __restrict__ table) {
+  __shared__ __attribute__((aligned(16))) Lds<D> red;
+  __shared__ __attribute__((aligned(16))) char params[4 * Long::kLds];
+  const Piece piece = piece_of(a.lens, a.B, a.cols, a.c.Hkv * a.tiles, a.units);
+  if (!piece.any) return;
+  if constexpr (!std::is_same<Form, Long>::value) {
+    if (piece.many) {
+      attend<D, Long>(a, table, piece, red, params);
+      return;
+    }
+  }
+  attend<D, Form>(a, table, piece, red, params);
+}
+
+// Workgroups that the pages are shared out to. Rounding a sequence's last piece up makes at most one more for each sequence and head; of those that are
+// cut there are at most twice as many pieces as shares.
+int attn_units() { return 2 * compute_units(); }
 
 }  // namespace
 
 size_t paged_attn_workspace(const PagedAttnView& a) {
   const int G = a.Hq / a.c.Hkv, columns = a.T * G < 16 ? a.T * G : 16;
   const size_t floats = a.c.d == 128 ? Slot<128>{columns}.floats() : Slot<64>{columns}.floats();
-  return (size_t)2 * attn_workgroups() * floats * sizeof(float);
+  return (size_t)2 * attn_units() * floats * sizeof(float);
 }
 
 hipError_t launch_paged_attn(const PagedAttnView& v, void* workspace, unsigned long long tag, hipStream_t s) {
-  const int G = v.Hq / v.c.Hkv, columns = v.T * G;
-  const Args a = {v.c, (const bf16_t*)v.q, (bf16_t*)v.o, v.lens, (float*)workspace, tag, v.B, v.cols, v.T, v.Hq, G, (columns + 15) / 16, v.scale};
-  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, dim3(attn_workgroups()), dim3(256), 0, s, a, v.table); };
-  if (v.c.dtype == YOCO_INT4) {
-    if (v.c.d == 128) columns <= 4 ? go(&attn_kernel<128, Coded<128, 4>>) : columns <= 8 ? go(&attn_kernel<128, Coded<128, 2>>) : go(&attn_kernel<128, Coded<128, 1>>);
-    else columns <= 4 ? go(&attn_kernel<64, Coded<64, 4>>) : columns <= 8 ? go(&attn_kernel<64, Coded<64, 2>>) : go(&attn_kernel<64, Coded<64, 1>>);
-  } else {
-    v.c.d == 128 ? go(&attn_kernel<128, Plain<128>>) : go(&attn_kernel<64, Plain<64>>);
-  }
+  const int G = v.Hq / v.c.Hkv, columns = v.T * G, tiles = (columns + 15) / 16, units = attn_units();
+  const Args a = {v.c, (const bf16_t*)v.q, (bf16_t*)v.o, v.lens, (float*)workspace, tag, v.B, v.cols, v.T, v.Hq, G, tiles, units, v.scale};
+  // no more pieces than pages
+  const int64_t segments = (int64_t)v.B * v.c.Hkv * tiles, most = segments * ((v.cols + kMinPages - 1) / kMinPages);
+  const dim3 grid((unsigned)(segments + units < most ? segments + units : most));
+  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, v.table); };
+  auto by_d = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    if (v.c.dtype != YOCO_INT4) go(&attn_kernel<D, Plain<D>, Plain<D>>);
+    else if (columns <= 4) go(&attn_kernel<D, Coded<D, 1>, Coded<D, 4>>);
+    else if (columns <= 8) go(&attn_kernel<D, Coded<D, 1>, Coded<D, 2>>);
+    else go(&attn_kernel<D, Coded<D, 1>, Coded<D, 1>>);
+  };
+  if (v.c.d == 128) by_d(std::integral_constant<int, 128>());
+  else by_d(std::integral_constant<int, 64>());
   return hipGetLastError();
 }
 

@@ -357,7 +357,7 @@ int check_table(const int32_t* table, int B, int cols) {
   if (!table) return fail(YOCO_ERR_INVALID_ARG, "table is null");
   if (B <= 0 || cols <= 0) return fail(YOCO_ERR_INVALID_ARG, "non-positive B or cols");
   if (B > 65535) return fail(YOCO_ERR_UNSUPPORTED, "B %d exceeds the grid limit", B);
-  if (cols > 1 << 24) return fail(YOCO_ERR_UNSUPPORTED, "cols %d exceeds 2^24", cols);
+  if (cols > 1 << 20) return fail(YOCO_ERR_UNSUPPORTED, "cols %d exceeds 2^20", cols);
   if (((uintptr_t)table) & 3u) return fail(YOCO_ERR_ALIGNMENT, "table is not 4-byte aligned");
   return YOCO_OK;
 }
