@@ -30,6 +30,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegBig = -1.0e30f;      // "no row seen yet": finite, so m - m never makes NaN
 constexpr int kMinPages = 16;            // of a workgroup, where there are more
 constexpr int kManyPages = 32;
+constexpr int kAhead4 = 2, kAhead2 = 4, kAheadPlain = 8;
 
 // What a workgroup takes: pages [p0, p1) of the P of a sequence, for a KV head (and column tile).
 struct Piece {
@@ -109,12 +110,20 @@ struct Args {
 };
 
 // What a wavefront knows of its columns (lane n = lane % 16): one softmax state for each lane n.
-template <int D>
+template <int D, int NP>
 struct State {
   float m, l;
   f32x4 o[D / 16];
   float z[D / 64];                       // 4 bits: sum of p * minimum, this lane's rows
-  unsigned e;                            // 4 bits: exponent field of the largest scale so far; o is relative to 2^(e - 126)
+  int e[NP];                             // 4 bits: exponent field of the largest scale of V that a bank's pages had; its o are relative to 2^(e - 126)
+};
+
+// Where the pages of a KV head are.
+struct Head {
+  const char *k, *v;
+  size_t apart;                          // bytes from a page to the next
+  __device__ __forceinline__ const char* k_of(int page) const { return k + (size_t)page * apart; }
+  __device__ __forceinline__ const char* v_of(int page) const { return v + (size_t)page * apart; }
 };
 
 __device__ __forceinline__ float exp2i(int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
@@ -132,17 +141,18 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
 }
 __device__ __forceinline__ u32x4 only(bool mine, u32x4 x) { return (u32x4){mine ? x[0] : 0u, mine ? x[1] : 0u, mine ? x[2] : 0u, mine ? x[3] : 0u}; }
 
-constexpr int kParamStride = 64 * 16 + 16;     // of a page's scales in LDS: the four pages of a read fall in distinct banks
+constexpr int kParamStride = 64 * 32 + 32;     // of a page's scales in LDS: the four pages of a read fall in distinct banks
 
-template <int D, int NP>
+template <int D, int NP, int R>
 struct Coded {
   static constexpr int kGroups = D / 64, kSteps = D / 32, kLoads = D / 32;        // 16-byte loads of a plane's page
   static constexpr int kPages = NP, kColumns = 16 / NP;
   static constexpr int kLds = NP * kParamStride;
-  static constexpr bool kApart = NP < 4; // K and V have registers of their own; else a page's are K's, then V's
-  struct Page {
-    u32x4 x[kLoads], y[kApart ? kLoads : 0];
-    unsigned k[kGroups], v[kGroups];     // row `lane`'s scales and minima
+  static constexpr int kPlanes = 2 * NP;                                          // of a step: K of its pages, then V
+  static_assert(kPlanes % R == 0, "a plane has its place among R in every step");
+  struct Pages {
+    u32x4 x[R][kLoads];                  // codes of plane i in x[i % R]; R planes are on their way
+    u32x2 k[NP], v[NP];                  // row `lane`'s scales and minima
   };
   struct Query {
     u32x4 f[kSteps];
@@ -153,21 +163,34 @@ struct Coded {
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) x[u] = __builtin_nontemporal_load((const u32x4*)at + u * 64 + lane);
   }
-  static __device__ __forceinline__ auto& codes_v(Page& p) {
-    if constexpr (kApart) return p.y;
-    else return p.x;
+  static __device__ __forceinline__ u32x2 params_of(const char* at, int lane) {
+    if (kGroups > 1) return ((const u32x2*)(at + 32 * D))[lane];
+    const unsigned one = ((const unsigned*)(at + 32 * D))[lane];
+    return (u32x2){one, one};
   }
-  static __device__ __forceinline__ void load_params(Page& p, const char* k, const char* v, int lane) {
+  static __device__ __forceinline__ void load_params(Pages& x, int j, const char* k, const char* v, int lane) {
+    x.k[j] = params_of(k, lane);
+    x.v[j] = params_of(v, lane);
+  }
+  // In the order of the loop: the scales of all pages, then codes.
+  static __device__ __forceinline__ void begin(Pages& x, const Head& head, const int (&now)[NP], int lane) {
 #pragma unroll
-    for (int h = 0; h < kGroups; ++h) {
-      p.k[h] = __builtin_nontemporal_load((const unsigned*)(k + 32 * D) + lane * kGroups + h);
-      p.v[h] = __builtin_nontemporal_load((const unsigned*)(v + 32 * D) + lane * kGroups + h);
+    for (int j = 0; j < NP; ++j) load_params(x, j, head.k_of(now[j]), head.v_of(now[j]), lane);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (i < NP) load(x.x[i], head.k_of(now[i % NP]), lane);
+      else load(x.x[i], head.v_of(now[i % NP]), lane);
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
-  static __device__ __forceinline__ void begin(Page& p, const char* k, const char* v, int lane) {
-    load(p.x, k, lane);
-    load_params(p, k, v, lane);
-    if (kApart) load(codes_v(p), v, lane);
+  // Plane i is done with: what comes R planes later takes its place, of this step or (MORE) of the next.
+  template <bool MORE>
+  static __device__ __forceinline__ void refill(Pages& x, int i, const Head& head, const int (&now)[NP], const int (&next)[NP], int lane) {
+    const int to = i + R;
+    if (to < NP) load(x.x[i % R], head.k_of(now[to % NP]), lane);
+    else if (to < kPlanes) load(x.x[i % R], head.v_of(now[to % NP]), lane);
+    else if (MORE && to < kPlanes + NP) load(x.x[i % R], head.k_of(next[to % NP]), lane);
+    else if (MORE) load(x.x[i % R], head.v_of(next[to % NP]), lane);
   }
 
   // raw[t]: dimensions 32 t + 8 qg .. of this lane's column. Numbers are scaled by a power of two so that the largest is in [2^14, 2^15).
@@ -205,24 +228,31 @@ struct Coded {
     q.c2 = most < 0x7f80u ? exp2i(down - half) : __uint_as_float(0x7fc00000u);                              // a query that is not finite
   }
 
-  // NP pages: this lane's column has the page of its bank (lane % 16 / kColumns), of whose rows it sees nv; rows[j]: rows that page j has. v: pages
-  // of V; k2, v2: of the next step (more). Four planes of pages, two of one, are on their way at any time.
-    static __device__ __forceinline__ void step(State<D>& st, const Query& q, Page (&x)[NP], int lane, int nv, const int (&rows)[NP], char* lds, bool more, const char* const (&v)[NP],
-                                              const char* const (&k2)[NP], const char* const (&v2)[NP]) {
+  // NP pages: this lane's column has the page of its bank (lane % 16 / kColumns), of whose rows it sees nv; rows[j]: rows that page j has. now: the pages;
+  // next: those of the next step (MORE).
+  template <bool MORE>
+  static __device__ __forceinline__ void step(State<D, kPages>& st, const Query& q, Pages& x, int lane, int nv, const int (&rows)[NP], char* lds, const Head& head,
+                                              const int (&now)[NP], const int (&next)[NP]) {
     const int qg = lane >> 4;
     int bank = (lane & 15) / kColumns;
     asm volatile("" : "+v"(bank));                                       // else the query is kept once for each bank: 64 registers
-    unsigned e_new = 0;
+    int e_old[NP];
+    bool larger = false;
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-      u32x4 par = {x[j].k[0], x[j].k[kGroups - 1], x[j].v[0], x[j].v[kGroups - 1]};
-      if (lane >= rows[j]) par = (u32x4){0u, 0u, 0u, 0u};        // whatever the memory held, NaN included
-      *(u32x4*)(lds + j * kParamStride + lane * 16) = par;
-      const unsigned e = (unsigned)lanes_max((int)((max(par[2] & 0x7f80u, par[3] & 0x7f80u)) >> 7));          // the page's largest scale
-      if (NP == 1 || bank == j) e_new = e;
-      if (more) load_params(x[j], k2[j], v2[j], lane);
+      u32x4 par = {x.k[j][0], x.k[j][1], x.v[j][0], x.v[j][1]};
+      if (lane >= rows[j]) par = (u32x4){0u, 0u, 0u, 0u};                // whatever the memory held, NaN included
+      const int e = lanes_max((int)(max(par[2] & 0x7f80u, par[3] & 0x7f80u) >> 7));
+      e_old[j] = st.e[j];
+      st.e[j] = e > st.e[j] ? e : st.e[j];
+      larger = larger || st.e[j] != e_old[j];                            // seldom
+      const float down = exp2i(126 - st.e[j]);                           // V's scales below 1
+      f32x4* const at = (f32x4*)(lds + j * kParamStride + lane * 32);
+      at[0] = (f32x4){__uint_as_float(par[0] << 16), __uint_as_float(par[0] & 0xffff0000u), __uint_as_float(par[1] << 16), __uint_as_float(par[1] & 0xffff0000u)};
+      at[1] = (f32x4){__uint_as_float(par[2] << 16) * down, __uint_as_float(par[2] & 0xffff0000u), __uint_as_float(par[3] << 16) * down, __uint_as_float(par[3] & 0xffff0000u)};
+      if (MORE) load_params(x, j, head.k_of(next[j]), head.v_of(next[j]), lane);
     }
-    e_new = max(e_new, st.e);
+    __builtin_amdgcn_sched_barrier(0);
     f32x4 acc[4][kGroups];
 #pragma unroll
     for (int tau = 0; tau < 4; ++tau)
@@ -238,57 +268,70 @@ struct Coded {
 #pragma unroll
         for (int t = 0; t < kSteps; ++t) {
           const int i = tau * kSteps + t;
-          acc[tau][t / 2] = mfma_f16(nibbles_k(x[j].x[i / 4][i % 4]), f[t], acc[tau][t / 2]);
+          acc[tau][t / 2] = mfma_f16(nibbles_k(x.x[j % R][i / 4][i % 4]), f[t], acc[tau][t / 2]);
         }
         __builtin_amdgcn_sched_barrier(0);                               // few operands at a time, and the loads go where the codes were
       }
-      if constexpr (!kApart) load(x[j].x, v[j], lane);
-      else if (more) load(x[j].x, k2[j], lane);
+      refill<MORE>(x, j, head, now, next, lane);
       __builtin_amdgcn_sched_barrier(0);
     }
     // scores of rows 16 tau + 4 qg + i of the bank's page
     float s[16], smax = -INFINITY;
-    const char* const mine = lds + bank * kParamStride + qg * 64;
+    const char* const mine = lds + bank * kParamStride + qg * 128;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int tau = r / 4, i = r % 4;
-      const u32x2 par = *(const u32x2*)(mine + (tau * 16 + i) * 16);
-      float a = 0.f;
+    for (int half = 0; half < 2; ++half) {
+      f32x4 par[8];
 #pragma unroll
-      for (int h = 0; h < kGroups; ++h) {
-        a = fmaf(__uint_as_float(par[h] << 16), acc[tau][h][i], a);
-        a = fmaf(__uint_as_float(par[h] & 0xffff0000u), q.sum[h], a);
+      for (int r = 0; r < 8; ++r) par[r] = *(const f32x4*)(mine + ((half * 2 + r / 4) * 16 + r % 4) * 32);
+      __builtin_amdgcn_sched_barrier(0);                                 // one wait for all
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        float a = par[r][1] * q.sum[0];
+        a = fmaf(par[r][0], acc[half * 2 + r / 4][0][r % 4], a);
+        if constexpr (kGroups > 1) {
+          a = fmaf(par[r][3], q.sum[1], a);
+          a = fmaf(par[r][2], acc[half * 2 + r / 4][1][r % 4], a);
+        }
+        s[half * 8 + r] = a * q.c1 * q.c2;
       }
-      a = a * q.c1 * q.c2;
-      if (tau * 16 + qg * 4 + i >= nv) a = -INFINITY;
-      s[r] = a;
-      smax = fmaxf(smax, a);
     }
+    if (__builtin_amdgcn_ballot_w64(nv < kPageRows)) {                   // the end of a sequence, or no page
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (r / 4 * 16 + qg * 4 + r % 4 >= nv) s[r] = -INFINITY;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) smax = fmaxf(smax, s[r]);
     const float m_new = fmaxf(st.m, over_rows<LaneMax>(smax));           // the four lanes of a column hold 16 rows each
-    if (__builtin_amdgcn_ballot_w64(m_new != st.m || e_new != st.e)) {   // rare once the stream has met its large scores
-      const float alpha = __builtin_amdgcn_exp2f(st.m - m_new), beta = __builtin_amdgcn_exp2f(st.m - m_new + (float)((int)st.e - (int)e_new));
+    if (larger || __builtin_amdgcn_ballot_w64(m_new != st.m)) {   // rare once the stream has met its large scores
+      int e = e_old[0] - st.e[0];
+#pragma unroll
+      for (int j = 1; j < NP; ++j)
+        if (const int other = __builtin_amdgcn_readfirstlane(e_old[j] - st.e[j]); bank == j) e = other;
+      const float alpha = __builtin_amdgcn_exp2f(st.m - m_new), beta = __builtin_amdgcn_exp2f(st.m - m_new + (float)e);
 #pragma unroll
       for (int t = 0; t < D / 16; ++t) st.o[t] *= beta;
 #pragma unroll
       for (int h = 0; h < kGroups; ++h) st.z[h] *= alpha;
       st.l *= alpha;
       st.m = m_new;
-      st.e = e_new;
     }
-    const float down = exp2i(126 - (int)e_new);                          // scales below 1
     u32x4 b[kGroups][2];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       float w[kGroups][8];
+      f32x4 par[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) par[r] = *(const f32x4*)(mine + ((half * 2 + r / 4) * 16 + r % 4) * 32 + 16);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
-        const float p = __builtin_amdgcn_exp2f(s[half * 8 + r] - m_new), pd = p * down;
-        const u32x2 par = *(const u32x2*)(mine + ((half * 2 + r / 4) * 16 + r % 4) * 16 + 8);
+        const float p = __builtin_amdgcn_exp2f(s[half * 8 + r] - m_new);
         st.l += p;
 #pragma unroll
         for (int h = 0; h < kGroups; ++h) {
-          st.z[h] = fmaf(p, __uint_as_float(par[h] & 0xffff0000u), st.z[h]);
-          w[h][r] = __uint_as_float(par[h] << 16) * pd;
+          w[h][r] = p * par[r][2 * h];
+          st.z[h] = fmaf(p, par[r][2 * h + 1], st.z[h]);
         }
       }
 #pragma unroll
@@ -306,20 +349,24 @@ struct Coded {
       for (int t = 0; t < kLoads; ++t) {                                 // 32 dimensions: the low nibbles are 16 of them, the high ones the others
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const unsigned w0 = codes_v(x[j])[t][half * 2], w1 = codes_v(x[j])[t][half * 2 + 1], u0 = w0 >> 8, u1 = w1 >> 8;
+          const unsigned w0 = x.x[(NP + j) % R][t][half * 2], w1 = x.x[(NP + j) % R][t][half * 2 + 1], u0 = w0 >> 8, u1 = w1 >> 8;
           st.o[2 * t] = mfma_f16((u32x4){w0 & 0x000f000fu, u0 & 0x000f000fu, w1 & 0x000f000fu, u1 & 0x000f000fu}, f[t / 2][half], st.o[2 * t]);
           st.o[2 * t + 1] = mfma_f16((u32x4){w0 & 0x00f000f0u, u0 & 0x00f000f0u, w1 & 0x00f000f0u, u1 & 0x00f000f0u}, f[t / 2][half], st.o[2 * t + 1]);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (more) load(codes_v(x[j]), kApart ? v2[j] : k2[j], lane);
+      refill<MORE>(x, NP + j, head, now, next, lane);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 
   // The state's vector as it is: dimensions 16 t + 4 qg + i.
-  static __device__ __forceinline__ void finish(State<D>& st) {
-    const float up = exp2i((int)st.e - 126 + 24);
+  static __device__ __forceinline__ void finish(State<D, kPages>& st, int bank) {
+    int e = st.e[0];
+#pragma unroll
+    for (int j = 1; j < NP; ++j)
+      if (const int other = __builtin_amdgcn_readfirstlane(st.e[j]); bank == j) e = other;
+    const float up = exp2i(e - 126 + 24);
 #pragma unroll
     for (int h = 0; h < kGroups; ++h) {
       const float z = over_rows<LaneSum>(st.z[h]);
@@ -332,28 +379,32 @@ struct Coded {
 };
 
 // ---- bf16 pages: softmax weights go in as a bf16 high part and a bf16 remainder (two products), which keeps 16 bits of them
-template <int D>
+template <int D, int R>
 struct Plain {
   static constexpr int kSteps = D / 32, kLoads = D / 8, kPages = 1, kColumns = 16, kLds = 16;
-  struct Page {
-    u32x4 x[kLoads];                     // K, then V
+  static_assert(kLoads % R == 0, "a piece has its place among R in either plane");
+  struct Pages {
+    u32x4 x[R];                          // 1 KiB pieces of K, then of V: piece i in x[i % R], R of them on their way
   };
   struct Query {
     u32x4 f[kSteps];
     float scale;
   };
   static __device__ __forceinline__ u32x4 piece(const char* at, int u, int lane) { return __builtin_nontemporal_load((const u32x4*)at + u * 64 + lane); }
-  static __device__ __forceinline__ void begin(Page& p, const char* k, const char*, int lane) {
+  static __device__ __forceinline__ void begin(Pages& x, const Head& head, const int (&now)[1], int lane) {
+    const char* const k = head.k_of(now[0]);
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) p.x[u] = piece(k, u, lane);
+    for (int u = 0; u < R; ++u) x.x[u] = piece(k, u, lane);
   }
   static __device__ __forceinline__ void prepare(Query& q, const u32x4 (&raw)[kSteps], float scale) {
 #pragma unroll
     for (int t = 0; t < kSteps; ++t) q.f[t] = raw[t];
     q.scale = scale * kLog2e;
   }
-    static __device__ __forceinline__ void step(State<D>& st, const Query& q, Page (&x)[1], int lane, int nv, const int (&rows)[1], char*, bool more, const char* const (&v)[1], const char* const (&k2)[1],
-                                              const char* const (&)[1]) {
+    template <bool MORE>
+  static __device__ __forceinline__ void step(State<D, kPages>& st, const Query& q, Pages& x, int lane, int nv, const int (&rows)[1], char*, const Head& head, const int (&now)[1],
+                                              const int (&next)[1]) {
+    const char *const k = head.k_of(now[0]), *const v = head.v_of(now[0]), *const k2 = head.k_of(next[0]);
     const int qg = lane >> 4;
     float s[16];
     float smax = -INFINITY;
@@ -362,8 +413,9 @@ struct Plain {
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int t = 0; t < kSteps; ++t) {
-        acc = mfma_bf16(x[0].x[tau * kSteps + t], q.f[t], acc);
-        x[0].x[tau * kSteps + t] = piece(v[0], tau * kSteps + t, lane);
+        const int i = tau * kSteps + t;
+        acc = mfma_bf16(x.x[i % R], q.f[t], acc);
+        x.x[i % R] = i + R < kLoads ? piece(k, i + R, lane) : piece(v, i + R - kLoads, lane);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -400,25 +452,32 @@ struct Plain {
     for (int t = 0; t < D / 16; ++t)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        u32x4& w = x[0].x[t * 2 + half];
-        w &= there[half];
+        const int i = t * 2 + half;
+        const u32x4 w = x.x[i % R] & there[half];
         st.o[t] = mfma_bf16(w, hi[half], st.o[t]);
         st.o[t] = mfma_bf16(w, lo[half], st.o[t]);
-        if (more) w = piece(k2[0], t * 2 + half, lane);
+        if (i + R < kLoads) x.x[i % R] = piece(v, i + R, lane);
+        else if (MORE) x.x[i % R] = piece(k2, i + R - kLoads, lane);
       }
   }
-  static __device__ __forceinline__ void finish(State<D>&) {}
+  static __device__ __forceinline__ void finish(State<D, 1>&, int) {}
 };
 
 __device__ __forceinline__ unsigned pair_bf16(float a, float b) { return (unsigned)f32_to_bf16(a) | ((unsigned)f32_to_bf16(b) << 16); }
 
 template <int D>
-struct Lds {
+struct Merge {
   float o[4][16][D + 4], ml[4][16][2];
+};
+// The states that are merged at the end lie where the scales of the pages were.
+template <int D, typename Form>
+union Lds {
+  char params[4 * Form::kLds];
+  Merge<D> red;
 };
 
 template <int D, typename Form>
-__device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict__ table, const Piece& piece, Lds<D>& red, char* params) {
+__device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict__ table, const Piece& piece, Merge<D>& red, char* params) {
   constexpr int NP = Form::kPages, NC = Form::kColumns;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int n = lane & 15, qg = lane >> 4, bank = n / NC;
@@ -439,56 +498,53 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
   }
 
   const int32_t* const row = table + (int64_t)b * a.cols;
-  const char* const kp = (const char*)a.c.k + (size_t)g * page_size;
-  const char* const vp = (const char*)a.c.v + (size_t)g * page_size;
-  const size_t step_bytes = page_size * a.c.Hkv;
-  typename Form::Page x[NP];
-  State<D> st;
+  const Head head = {(const char*)a.c.k + (size_t)g * page_size, (const char*)a.c.v + (size_t)g * page_size, page_size * a.c.Hkv};
+  typename Form::Pages x;
+  State<D, NP> st;
   st.m = kNegBig;
   st.l = 0.f;
-  st.e = 0;
+#pragma unroll
+  for (int j = 0; j < NP; ++j) st.e[j] = 0;
 #pragma unroll
   for (int t = 0; t < D / 16; ++t) st.o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int h = 0; h < D / 64; ++h) st.z[h] = 0.f;
 
-  int first = piece.p0 + wave;
-  const char *v[NP], *k2[NP], *v2[NP];
-  int rows[NP], rows2[NP];                                               // -1: no such page
-  auto find = [&](int from, const char* (&k)[NP], const char* (&v)[NP], int (&rows)[NP]) {
+  typename Form::Query q;
+  Form::prepare(q, raw, a.scale);
+  // A wavefront's pages, 64 at a time: a lane has the entry of the table for one of them. In the loop nothing is loaded under a
+  // condition, so that every wait is for the oldest loads alone.
+  for (int p0 = piece.p0 + wave; p0 < p1; p0 += 256) {
+    const int mine = p0 + 4 * lane, id = row[mine < p1 ? mine : p1 - 1], left = len - mine * kPageRows;
+    const bool is = mine < p1 && id >= 0 && id < a.c.n_pages;
+    const int page = is ? id : 0, has = is ? left < kPageRows ? left : kPageRows : -1;       // -1: no such page
+    const int count = (p1 - p0 + 3) / 4 < 64 ? (p1 - p0 + 3) / 4 : 64;
+    int now[NP], next[NP], rows[NP], nv;
 #pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      const int p = from + 4 * j, id = row[p < p1 ? p : p1 - 1], left = len - p * kPageRows;
-      const bool is = p < p1 && id >= 0 && id < a.c.n_pages;
-      rows[j] = is ? left < kPageRows ? left : kPageRows : -1;
-      k[j] = kp + (is ? id : 0) * step_bytes;
-      v[j] = vp + (is ? id : 0) * step_bytes;
-    }
-  };
-  if (first < p1) {
-    find(first, k2, v, rows);
-#pragma unroll
-    for (int j = 0; j < NP; ++j) Form::begin(x[j], k2[j], v[j], lane);
-    typename Form::Query q;
-    Form::prepare(q, raw, a.scale);
-    while (first < p1) {
-      int nv = 0;                                                        // rows of its bank's page that this lane's column sees
-#pragma unroll
-      for (int j = 0; j < NP; ++j)
-        if (NP == 1 || bank == j) nv = rows[j] < 0 ? 0 : seen - (first + 4 * j) * kPageRows;
-      first += 4 * NP;
-      const bool more = first < p1;
-      if (more) find(first, k2, v2, rows2);
-      Form::step(st, q, x, lane, nv, rows, params + wave * Form::kLds, more, v, k2, v2);
+    for (int j = 0; j < NP; ++j) now[j] = __builtin_amdgcn_readlane(page, j);
+    Form::begin(x, head, now, lane);
+    auto look = [&](int i) {                                             // rows of the pages, and what this lane's column sees of its bank's
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
-        v[j] = v2[j];
-        rows[j] = rows2[j];
+        rows[j] = __builtin_amdgcn_readlane(has, i + j);
+        if (NP == 1 || bank == j) nv = rows[j] < 0 ? 0 : seen - (p0 + 4 * (i + j)) * kPageRows;
       }
+    };
+    int i = 0;
+    for (; i + NP < count; i += NP) {
+#pragma unroll
+      for (int j = 0; j < NP; ++j) next[j] = __builtin_amdgcn_readlane(page, i + NP + j);
+      look(i);
+      Form::template step<true>(st, q, x, lane, nv, rows, params + wave * Form::kLds, head, now, next);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) now[j] = next[j];
     }
+    look(i);
+    Form::template step<false>(st, q, x, lane, nv, rows, params + wave * Form::kLds, head, now, now);
   }
-  Form::finish(st);
+  Form::finish(st, bank);
   const float l = over_rows<LaneSum>(st.l);
+  __syncthreads();
 #pragma unroll
   for (int t = 0; t < D / 16; ++t) *(f32x4*)&red.o[wave][n][t * 16 + qg * 4] = st.o[t];
   if (qg == 0) {
@@ -574,17 +630,16 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
 // Long: the form where a wavefront has many pages.
 template <int D, typename Form, typename Long>
 __global__ void __launch_bounds__(256, 2) attn_kernel(Args a, const int32_t* __restrict__ table) {
-  __shared__ __attribute__((aligned(16))) Lds<D> red;
-  __shared__ __attribute__((aligned(16))) char params[4 * Long::kLds];
+  __shared__ __attribute__((aligned(16))) Lds<D, Long> lds;
   const Piece piece = piece_of(a.lens, a.B, a.cols, a.c.Hkv * a.tiles, a.units);
   if (!piece.any) return;
   if constexpr (!std::is_same<Form, Long>::value) {
     if (piece.many) {
-      attend<D, Long>(a, table, piece, red, params);
+      attend<D, Long>(a, table, piece, lds.red, lds.params);
       return;
     }
   }
-  attend<D, Form>(a, table, piece, red, params);
+  attend<D, Form>(a, table, piece, lds.red, lds.params);
 }
 
 // Workgroups that the pages are shared out to. Rounding a sequence's last piece up makes at most one more for each sequence and head; of those that are
@@ -608,10 +663,10 @@ hipError_t launch_paged_attn(const PagedAttnView& v, void* workspace, unsigned l
   auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, v.table); };
   auto by_d = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (v.c.dtype != YOCO_INT4) go(&attn_kernel<D, Plain<D>, Plain<D>>);
-    else if (columns <= 4) go(&attn_kernel<D, Coded<D, 1>, Coded<D, 4>>);
-    else if (columns <= 8) go(&attn_kernel<D, Coded<D, 1>, Coded<D, 2>>);
-    else go(&attn_kernel<D, Coded<D, 1>, Coded<D, 1>>);
+    if (v.c.dtype != YOCO_INT4) go(&attn_kernel<D, Plain<D, kAheadPlain>, Plain<D, kAheadPlain>>);
+    else if (columns <= 4) go(&attn_kernel<D, Coded<D, 1, 2>, Coded<D, 4, kAhead4>>);
+    else if (columns <= 8) go(&attn_kernel<D, Coded<D, 1, 2>, Coded<D, 2, kAhead2>>);
+    else go(&attn_kernel<D, Coded<D, 1, 2>, Coded<D, 1, 2>>);
   };
   if (v.c.d == 128) by_d(std::integral_constant<int, 128>());
   else by_d(std::integral_constant<int, 64>());
