@@ -32,63 +32,119 @@ constexpr int kMinPages = 16;            // of a workgroup, where there are more
 constexpr int kManyPages = 32;
 constexpr int kAhead4 = 2, kAhead2 = 4, kAheadPlain = 8;
 
-// What a workgroup takes: pages [p0, p1) of the P of a sequence, for a KV head (and column tile).
+// What a workgroup takes: pages [p0, p1) of a sequence, for a KV head (and column tile).
 struct Piece {
   int b, head, len, p0, p1;
-  int part, parts, slot;                 // which of the pieces of this sequence and head, how many, and the first one's place in the workspace
-  bool any, many;                        // many: a wavefront has several steps of four pages
+  int part, parts;                       // which of the pieces of this sequence and head, and how many
+  int slot;                              // the first one's place in the workspace, ...
+  bool ranges;                           // ... or the first workgroup that has one, and each has two places: for what ends at its range's beginning, and what begins at its end
 };
 
 __device__ __forceinline__ int up_to(int x, int by) { return (x + by - 1) / by * by; }
 
-// Every workgroup cuts the same lengths the same way, 64 sequences at a time, one a lane, and takes the piece of its number.
-__device__ __forceinline__ Piece piece_of(const int64_t* lens, int B, int cols, int heads, int units) {
-  const int lane = threadIdx.x & 63;
-  int len = 0, pages = 0;
-  auto look = [&](int at) {
-    const int64_t most = (int64_t)cols * kPageRows, n = at + lane < B ? lens[at + lane] : 0;
+// The pages of a batch, shared out; every workgroup does so alike. Sequences are looked at 64 at a time, one a lane.
+struct Shares {
+  const int64_t* lens;
+  int B, cols, heads, units;             // heads: KV heads x column tiles; units: workgroups to share the pages out to
+  int first, len, pages;                 // the 64 that are looked at, and this lane's
+  int total;                             // pages of all heads
+  __device__ __forceinline__ void look(int at) {
+    const int i = at + (int)(threadIdx.x & 63);
+    const int64_t most = (int64_t)cols * kPageRows, n = i < B ? lens[i] : 0;
+    first = at;
     len = (int)(n < 0 ? 0 : n > most ? most : n);
     pages = (len + kPageRows - 1) / kPageRows;
-  };
-  int total = 0;
-  for (int at = 0; at < B; at += 64) {
-    look(at);
-    total += lanes_sum(pages);
   }
-  Piece x = {};
-  int share = total * heads / units + 1;
-  x.many = share >= kManyPages;
-  const int grain = x.many ? 16 : 4;
-  share = share < kMinPages ? kMinPages : up_to(share, grain);
-  int id = blockIdx.x, slots = 0;
-  for (int at = 0; at < B; at += 64) {
-    if (B > 64) look(at);
-    const int wanted = pages > share ? about_ceil_div(pages, share) : 1;
-    const int each = up_to(about_ceil_div(pages + 1, wanted), grain);    // + 1: above 0
-    const int n = pages > each ? about_ceil_div(pages, each) : 1;
-    const int count = at + lane < B ? n * heads : 0, split = n > 1 ? count : 0;
-    const auto plus = [](int a, int b) { return a + b; };
-    const int upto = lane_scan(count, plus), slots_upto = lane_scan(split, plus);
-    if (id < last_lane(upto)) {
-      const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(id < upto));
-      x.any = true;
-      x.b = at + i;
-      x.len = __builtin_amdgcn_readlane(len, i);
-      x.parts = __builtin_amdgcn_readlane(n, i);
-      const int mine = id - __builtin_amdgcn_readlane(upto - count, i), size = __builtin_amdgcn_readlane(each, i);
-      x.head = __builtin_amdgcn_readfirstlane(mine / x.parts);
-      x.part = mine - x.head * x.parts;
-      x.slot = slots + __builtin_amdgcn_readlane(slots_upto - split, i) + x.head * x.parts;
-      const int P = __builtin_amdgcn_readlane(pages, i);
-      x.p0 = x.part * size;
-      x.p1 = x.p0 + size < P ? x.p0 + size : P;
-      return x;
+  __device__ __forceinline__ Shares(const int64_t* lens, int B, int cols, int heads, int units) : lens(lens), B(B), cols(cols), heads(heads), units(units) {
+    total = 0;
+    for (int at = 0; at < B; at += 64) {
+      look(at);
+      total += lanes_sum(pages);
     }
-    id -= last_lane(upto);
-    slots += last_lane(slots_upto);
+    total *= heads;
+    if (B > 64) look(0);
   }
-  return x;
-}
+  // Ranges where both a range and a sequence have many pages.
+  __device__ __forceinline__ bool ranges() const { return total / units >= kManyPages && total / (B * heads) >= 2 * kManyPages; }
+  static __device__ __forceinline__ int scan(int x) {
+    return lane_scan(x, [](int a, int b) { return a + b; });
+  }
+
+  // Few pages: a workgroup has one piece, and pieces end with their sequence, because a second beginning costs as much as many pages.
+  __device__ __forceinline__ bool piece(int id, Piece& x) {
+    const int lane = threadIdx.x & 63, grain = 4;
+    int share = total / units + 1, each = 0, n = 0, slots = 0;
+    share = share < kMinPages ? kMinPages : up_to(share, grain);
+    auto cut = [&] {
+      const int wanted = pages > share ? about_ceil_div(pages, share) : 1;
+      each = up_to(about_ceil_div(pages + 1, wanted), grain);              // + 1: above 0
+      n = pages > each ? about_ceil_div(pages, each) : 1;
+    };
+    // No more pieces than places at once, where that can be had: the ones that are too many would start when others are done.
+    if (B <= 64 && B * heads < units)
+      for (int i = 0; i < 16; ++i) {
+        cut();
+        const int over = lanes_sum(lane < B ? n : 0) * heads - units;
+        if (over <= 0) break;
+        share = up_to(share + share * over / units / 2 + 1, grain);
+      }
+    for (int at = 0; at < B; at += 64) {
+      if (B > 64) look(at);
+      cut();
+      const int count = at + lane < B ? n * heads : 0, split = n > 1 ? count : 0, upto = scan(count), slots_upto = scan(split);
+      if (id < last_lane(upto)) {
+        const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(id < upto));
+        const int mine = id - __builtin_amdgcn_readlane(upto - count, i), size = __builtin_amdgcn_readlane(each, i), P = __builtin_amdgcn_readlane(pages, i);
+        x.parts = __builtin_amdgcn_readlane(n, i);
+        x.b = at + i;
+        x.len = __builtin_amdgcn_readlane(len, i);
+        x.head = __builtin_amdgcn_readfirstlane(mine / x.parts);
+        x.part = mine - x.head * x.parts;
+        x.slot = slots + __builtin_amdgcn_readlane(slots_upto - split, i) + x.head * x.parts;
+        x.ranges = false;
+        x.p0 = x.part * size;
+        x.p1 = x.p0 + size < P ? x.p0 + size : P;
+        return true;
+      }
+      id -= last_lane(upto);
+      slots += last_lane(slots_upto);
+    }
+    return false;
+  }
+
+  // Many: all pages in a row, cut into as many equal ranges as there are workgroups, so that they end together.
+  __device__ __forceinline__ int begin(int w) const {
+    const int each = total / units, more = total - each * units;
+    return w * each + (w < more ? w : more);
+  }
+  __device__ __forceinline__ int owner(int u) const {
+    const int each = total / units, more = total - each * units, big = more * (each + 1);
+    return u < big ? u / (each + 1) : more + (u - big) / each;
+  }
+  // The piece that begins at page u of a range that ends at `end`; `before`: pages before the 64 sequences that are looked at.
+  __device__ __forceinline__ Piece piece_at(int u, int end, int& before) {
+    int upto = scan(pages);
+    while (u >= before + last_lane(upto) * heads) {
+      before += last_lane(upto) * heads;
+      look(first + 64);
+      upto = scan(pages);
+    }
+    const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(u < before + upto * heads));
+    const int P = __builtin_amdgcn_readlane(pages, i), seq0 = before + (__builtin_amdgcn_readlane(upto, i) - P) * heads;
+    Piece x;
+    x.b = first + i;
+    x.len = __builtin_amdgcn_readlane(len, i);
+    x.head = __builtin_amdgcn_readfirstlane((u - seq0) / P);
+    const int seg0 = seq0 + x.head * P;
+    x.p0 = u - seg0;
+    x.p1 = end - seg0 < P ? end - seg0 : P;
+    x.ranges = true;
+    x.slot = __builtin_amdgcn_readfirstlane(owner(seg0));
+    x.parts = __builtin_amdgcn_readfirstlane(owner(seg0 + P - 1)) - x.slot + 1;
+    x.part = (int)blockIdx.x - x.slot;
+    return x;
+  }
+};
 
 template <int D>
 struct Slot {                            // of a partial result: vectors, then (max, sum), then a tag for each wavefront
@@ -556,7 +612,7 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
   // A wavefront has every fourth column to itself: it merges the wavefronts' and banks' states, and publishes its part or, where it finds
   // all parts published, merges those.
   const int parts = piece.parts, e = lane * 2;
-  auto place = [&](int i) { return a.ws + (size_t)(piece.slot + i) * slot.floats(); };
+  auto place = [&](int i) { return a.ws + (size_t)(piece.ranges ? 2 * (piece.slot + i) + (i == 0) : piece.slot + i) * slot.floats(); };
   float* const mine = place(piece.part);
   auto store = [&](int c, float o0, float o1, float sum) {               // no row seen: zeros
     if (e >= D) return;
@@ -631,31 +687,46 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
 template <int D, typename Form, typename Long>
 __global__ void __launch_bounds__(256, 2) attn_kernel(Args a, const int32_t* __restrict__ table) {
   __shared__ __attribute__((aligned(16))) Lds<D, Long> lds;
-  const Piece piece = piece_of(a.lens, a.B, a.cols, a.c.Hkv * a.tiles, a.units);
-  if (!piece.any) return;
-  if constexpr (!std::is_same<Form, Long>::value) {
-    if (piece.many) {
-      attend<D, Long>(a, table, piece, lds.red, lds.params);
-      return;
-    }
+  Shares shares(a.lens, a.B, a.cols, a.c.Hkv * a.tiles, a.units);
+  const int me = blockIdx.x;
+  const bool ranges = shares.ranges();
+  Piece piece;
+  int u = 0, end = 1, before = 0;
+  if (ranges) {
+    const int row = a.T * a.Hq * (D / 2);                                // a sequence without rows is in no range: its outputs are zeros
+    for (int b = me; b < a.B; b += gridDim.x)
+      if (a.lens[b] <= 0)
+        for (int i = threadIdx.x; i < row; i += 256) ((unsigned*)a.o)[(int64_t)b * row + i] = 0;
+    if (me >= a.units) return;
+    u = shares.begin(me);
+    end = shares.begin(me + 1);
+  } else if (!shares.piece(me, piece)) {
+    return;
   }
-  attend<D, Form>(a, table, piece, lds.red, lds.params);
+  while (u < end) {
+    if (ranges) piece = shares.piece_at(u, end, before);
+    const int pages = piece.p1 - piece.p0;
+    u += ranges ? pages : 1;
+    if (!std::is_same<Form, Long>::value && pages >= kManyPages) attend<D, Long>(a, table, piece, lds.red, lds.params);
+    else attend<D, Form>(a, table, piece, lds.red, lds.params);
+    __syncthreads();                                                     // what the merge has read is written again
+  }
 }
 
 // Workgroups that the pages are shared out to. Rounding a sequence's last piece up makes at most one more for each sequence and head; of those that are
 // cut there are at most twice as many pieces as shares.
-int attn_units() { return 2 * compute_units(); }
+int attn_units(int dtype) { return dtype == YOCO_INT4 ? 2 * compute_units() : compute_units(); }
 
 }  // namespace
 
 size_t paged_attn_workspace(const PagedAttnView& a) {
   const int G = a.Hq / a.c.Hkv, columns = a.T * G < 16 ? a.T * G : 16;
   const size_t floats = a.c.d == 128 ? Slot<128>{columns}.floats() : Slot<64>{columns}.floats();
-  return (size_t)2 * attn_units() * floats * sizeof(float);
+  return (size_t)2 * attn_units(a.c.dtype) * floats * sizeof(float);
 }
 
 hipError_t launch_paged_attn(const PagedAttnView& v, void* workspace, unsigned long long tag, hipStream_t s) {
-  const int G = v.Hq / v.c.Hkv, columns = v.T * G, tiles = (columns + 15) / 16, units = attn_units();
+  const int G = v.Hq / v.c.Hkv, columns = v.T * G, tiles = (columns + 15) / 16, units = attn_units(v.c.dtype);
   const Args a = {v.c, (const bf16_t*)v.q, (bf16_t*)v.o, v.lens, (float*)workspace, tag, v.B, v.cols, v.T, v.Hq, G, tiles, units, v.scale};
   // no more pieces than pages
   const int64_t segments = (int64_t)v.B * v.c.Hkv * tiles, most = segments * ((v.cols + kMinPages - 1) / kMinPages);
