@@ -387,9 +387,9 @@ def paged_append(cache, table, pos, k, v, rows=None, q=None, turns=None, neighbo
 
 def paged_read(cache, table, pos, T, dtype=torch.bfloat16):
     """The values of rows pos[b] .. pos[b] + T - 1: k, v [B,T,Hkv,d] (yoco_paged_read)."""
-    k, v = (torch.empty((table.shape[0], T, cache.Hkv, cache.d), dtype=dtype, device=table.device) for _ in range(2))
-    (_CALLS or _calls()).paged_read(cache.address, table, pos, T, k, v)
-    return k, v
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise YocoError("rows are read as float32 or bfloat16, not %s" % dtype)
+    return (_CALLS or _calls()).paged_read(cache.address, table, pos, T, dtype is torch.bfloat16)
 
 
 def paged_attn_workspace(cache, B, columns, T, Hq):

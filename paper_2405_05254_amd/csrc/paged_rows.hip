@@ -1,16 +1,20 @@
-// Rows into pages and back: the rotation to their positions, the 4-bit coding, and the order inside a page.
+// Rows into pages and back: the rotation to their positions, the 4-bit coding, and the order inside a page. Bound by memory where rows are
+// many, by the launch where they are few.
 //
-// A row of a head is d / 8 threads with 8 dimensions each, and the threads of a workgroup are 2048 / d such rows. The angle of
-// a pair at a position is a whole number of 2^-64 turns times the position, wrapped: exact wherever the position is. Cosine and
-// sine of its upper 32 bits are formed once for a row and workgroup, because all heads share them.
+// A workgroup has the 16 rows of a page that lie together in the operands (of which a call may bring fewer), and all heads of
+// them or a part. The angle of a pair at a position is a whole number of 2^-64 turns times the position, wrapped: exact wherever the
+// position is. Cosine and sine of its upper 32 bits are formed once for a row and workgroup, because all heads share them. A row
+// of a head is d / 16 threads with two pieces of 8 dimensions each: the two that are rotated with each other (K, Q), or those whose
+// codes share bytes (V). V lies transposed in a page; of 16 rows it goes through LDS, because bytes scattered over the page take
+// eight times as many stores.
 #include "lanes.h"
+#include "mfma_util.h"
 #include "paged.h"
 
 namespace yoco {
 
 namespace {
 
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 struct LaneMin {
@@ -38,10 +42,7 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   for (int i = 0; i < 2; ++i) *(f32x4*)(p + 4 * i) = (f32x4){x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
 }
 __device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {
-  u32x4 a;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) a[j] = (unsigned)f32_to_bf16(x[2 * j]) | ((unsigned)f32_to_bf16(x[2 * j + 1]) << 16);
-  *(u32x4*)p = a;
+  *(u32x4*)p = (u32x4){pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
 }
 
 // Cosine and sine of pair p at a position: the upper 32 bits of the phase are a signed part of a turn.
@@ -60,115 +61,234 @@ __device__ __forceinline__ float turned(float x, float y, float c, float s) {   
   return a + b;
 }
 
-// Dimensions e0 .. e0 + 7 of a row, rotated; src points at the row's head.
-template <typename S>
-__device__ __forceinline__ void rotated(const S* src, int e0, int rot, int neighbours, const float2* cs, float (&x)[8]) {
-  load8(src + e0, x);
-  if (e0 >= rot) return;                                                            // rot is a multiple of 16
-  if (neighbours) {
+// Two pieces of 8 dimensions, rotated where they lie below `rot`, a multiple of 16: with each other, or each in itself.
+__device__ __forceinline__ void rotate(float (&x)[8], float (&y)[8], int e0, int e1, int rot, int neighbours, const float2* cs) {
+  if (!neighbours) {
+    if (e0 >= rot) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 t = cs[e0 / 2 + j];
-      const float a = x[2 * j], b = x[2 * j + 1];
-      x[2 * j] = turned(a, b, t.x, -t.y);
-      x[2 * j + 1] = turned(b, a, t.x, t.y);
+    for (int j = 0; j < 8; ++j) {
+      const float2 t = cs[e0 + j];
+      const float a = x[j], b = y[j];
+      x[j] = turned(a, b, t.x, -t.y);
+      y[j] = turned(b, a, t.x, t.y);
     }
     return;
   }
-  const int half = rot / 2, p0 = e0 < half ? e0 : e0 - half;
-  float y[8];
-  load8(src + (e0 < half ? e0 + half : p0), y);
+  auto one = [&](float(&z)[8], int e) {
+    if (e >= rot) return;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float2 t = cs[p0 + j];
-    x[j] = turned(x[j], y[j], t.x, e0 < half ? -t.y : t.y);
-  }
+    for (int j = 0; j < 4; ++j) {
+      const float2 t = cs[e / 2 + j];
+      const float a = z[2 * j], b = z[2 * j + 1];
+      z[2 * j] = turned(a, b, t.x, -t.y);
+      z[2 * j + 1] = turned(b, a, t.x, t.y);
+    }
+  };
+  one(x, e0);
+  one(y, e1);
 }
 
-// The codes of 8 of a group's 64 dimensions, its 8 threads side by side: 4 bits each, lowest dimension first. `param`: bf16 scale and minimum.
-// A group that holds what is not finite, or whose range is not, stands for NaN.
-__device__ __forceinline__ unsigned code8(const float (&x)[8], unsigned& param) {
-#pragma clang fp contract(off)
-  float lo = x[0], hi = x[0];
-  unsigned bad = 0;
+// What 64 dimensions that share a scale have in common.
+struct Group {
+  float lo = INFINITY, hi = -INFINITY, bad = 0.f;
+  __device__ __forceinline__ void see(const float (&x)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    lo = fminf(lo, x[j]);
-    hi = fmaxf(hi, x[j]);
-    bad |= not_finite(x[j]);
+    for (int j = 0; j < 8; ++j) {
+      lo = fminf(lo, x[j]);
+      hi = fmaxf(hi, x[j]);
+      bad = not_finite(x[j]) ? 1.f : bad;
+    }
   }
-  float b = (float)bad;
-  lo = over8<LaneMin>(lo);
-  hi = over8<LaneMax>(hi);
-  b = over8<LaneMax>(b);
-  const float range = hi - lo;
-  const unsigned base = f32_to_bf16(lo);
-  unsigned scale = f32_to_bf16(range * (float)(1.0 / 15.0));
-  if (scale < 0x0080u) scale = 0;                                                   // below the normal numbers: all of one value
-  if (b > 0.f || not_finite(range) || (scale & 0x7f80u) == 0x7f80u || (base & 0x7f80u) == 0x7f80u) {
-    param = 0x7fc00000u;                                                            // scale 0, minimum NaN
-    return 0;
+  template <int THREADS>                             // that hold the row of a head, side by side
+  __device__ __forceinline__ void join() {
+    if (THREADS == 8) {
+      lo = over8<LaneMin>(lo);
+      hi = over8<LaneMax>(hi);
+      bad = over8<LaneMax>(bad);
+    } else {
+      lo = over4<LaneMin>(lo);
+      hi = over4<LaneMax>(hi);
+      bad = over4<LaneMax>(bad);
+    }
   }
-  param = scale | (base << 16);
-  const float s = __uint_as_float(scale << 16), base_f = __uint_as_float(base << 16), inv = scale ? 1.f / s : 0.f;
+  // bf16 scale and minimum; what is not finite, or whose range is not, stands for NaN
+  __device__ __forceinline__ unsigned param() const {
+#pragma clang fp contract(off)
+    const float range = hi - lo;
+    const unsigned base = f32_to_bf16(lo);
+    unsigned scale = f32_to_bf16(range * (float)(1.0 / 15.0));
+    if (scale < 0x0080u) scale = 0;                  // below the normal numbers: all of one value
+    if (bad > 0.f || not_finite(range) || (scale & 0x7f80u) == 0x7f80u || (base & 0x7f80u) == 0x7f80u) return 0x7fc00000u;      // scale 0, minimum NaN
+    return scale | (base << 16);
+  }
+};
+// The codes of 8 dimensions, 4 bits each, lowest dimension first.
+__device__ __forceinline__ unsigned code8(const float (&x)[8], unsigned param) {
+#pragma clang fp contract(off)
+  const float s = __uint_as_float(param << 16), base = __uint_as_float(param & 0xffff0000u), inv = (param & 0xffffu) ? 1.f / s : 0.f;
   unsigned codes = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float y = (x[j] - base_f) * inv;
+    const float y = (x[j] - base) * inv;
     codes |= (unsigned)(int)fminf(fmaxf(rintf(y), 0.f), 15.f) << (4 * j);
   }
-  return codes;
+  return param == 0x7fc00000u ? 0u : codes;
 }
 
-// One new row a workgroup, and 2048 / d of its heads: queries, then keys, then values.
+constexpr int kTileRows = 16;
+
+// Which 16 rows workgroup x of n has. The four groups of a page share its cache lines (4 bytes of 16 in the V plane), and workgroups are dealt to
+// the 8 XCDs in turn: of 32 workgroups the four of a page are 8 apart, and meet in one L2.
+__device__ __forceinline__ int tile_of(int x, int n) { return (x | 31) < n ? (x & ~31) + x % 8 * 4 + x / 8 % 4 : x; }
+
 template <typename S, int D, bool CODED>
-__global__ void __launch_bounds__(256) append_kernel(AppendView a) {
-  __shared__ float2 cs[64];
-  constexpr int kThreads = D / 8, kHeads = 256 / kThreads;
-  const int64_t row = blockIdx.x;
-  const int b = (int)(row / a.T);
-  const int64_t t = row - (int64_t)b * a.T, pos = a.pos[b] + t;
-  if ((int)threadIdx.x < a.rot / 2) cs[threadIdx.x] = turn_of(a.turns[threadIdx.x], pos);
-  __syncthreads();
-  const int item = blockIdx.y * kHeads + threadIdx.x / kThreads, e0 = threadIdx.x % kThreads * 8;
-  if (item >= a.Hq + 2 * a.c.Hkv) return;
-  float x[8];
-  if (item < a.Hq) {
-    rotated((const S*)a.q + row * a.q_stride + (int64_t)item * D, e0, a.rot, a.neighbours, cs, x);
-    store8((S*)a.q_out + (row * a.Hq + item) * D + e0, x);
-    return;
+__global__ void __launch_bounds__(256) append_kernel(AppendView a, int tiles, int share) {
+  constexpr int kThreads = D / 16, kSlots = 256 / kThreads, kGroups = D / 64;
+  constexpr int kPlane = kTileRows * D / (CODED ? 2 : 1) * (CODED ? 1 : 2);      // bytes of 16 rows of a head in the V plane
+  __shared__ float2 cs[kTileRows][D / 2 + 1];
+  __shared__ __attribute__((aligned(16))) unsigned char turn[kSlots / kTileRows][kPlane];
+  const int group = tile_of(blockIdx.x, gridDim.x), b = group / tiles, tile = group - b * tiles;
+  const int64_t pos0 = a.pos[b], at = (pos0 & ~(int64_t)(kTileRows - 1)) + (int64_t)tile * kTileRows;     // first position of the 16 (floor: also below 0)
+  const int64_t n = a.rows ? (a.rows[b] < a.T ? a.rows[b] : a.T) : a.T;          // rows that are new
+  int t0 = (int)(at - pos0);                                                      // the row of the call at the first position
+  const int r0 = t0 < 0 ? -t0 : 0, r1 = a.T - t0 < kTileRows ? (int)(a.T - t0) : kTileRows, nr = r1 - r0;
+  if (nr <= 0) return;
+  const int slot = threadIdx.x / kThreads, th = threadIdx.x % kThreads;
+  // this thread's pieces: of K and Q the two that turn with each other, behind those (and of neighbours) any two; of V those that share bytes
+  const int half = a.neighbours ? 0 : a.rot / 16;
+  const int c0 = (th < half ? th : 2 * th) * 8, c1 = th < half ? c0 + a.rot / 2 : c0 + 8;
+  const int v0 = (th / 2 * 4 + th % 2) * 8, v1 = v0 + 16;
+
+  // [first, last) of all heads of Q, K and V. Of 16 rows V comes behind the others.
+  const bool whole = nr == kTileRows && t0 + kTileRows <= n;
+  const int keys = a.Hq, values = a.Hq + a.c.Hkv, heads = values + a.c.Hkv;
+  const int first = blockIdx.y * share, last = first + share < heads ? first + share : heads, last1 = whole && last > values ? values : last;
+  auto row_of = [&](int r) { return (int64_t)b * a.T + t0 + r; };
+  auto source = [&](int h, int r) {
+    const int64_t row = row_of(r);
+    return h < keys ? (const S*)a.q + row * a.q_stride + (int64_t)h * D : h < values ? (const S*)a.k + row * a.k_stride + (int64_t)(h - keys) * D : (const S*)a.v + row * a.v_stride + (int64_t)(h - values) * D;
+  };
+  int i = first * nr + slot;
+  float x[8], y[8];
+  auto fetch = [&](int i, float(&x)[8], float(&y)[8]) {
+    const int h = i / nr;
+    const S* const p = source(h, r0 + i - h * nr);
+    load8(p + (h < values ? c0 : v0), x);
+    load8(p + (h < values ? c1 : v1), y);
+  };
+  if (i < last1 * nr) fetch(i, x, y);                                             // on their way while the angles are formed
+  const int pairs = first < values ? a.rot / 2 : 0;
+  for (int k = threadIdx.x; k < nr * pairs; k += 256) {
+    const int r = k / pairs, p = k - r * pairs;
+    cs[r0 + r][p] = turn_of(a.turns[p], at + r0 + r);
   }
-  if (a.rows && t >= a.rows[b]) return;
-  if (pos < 0 || pos >= (int64_t)a.cols * kPageRows) return;
-  const int page = a.table[(int64_t)b * a.cols + pos / kPageRows];
-  if (page < 0 || page >= a.c.n_pages) return;
-  const int g = item - a.Hq, r = (int)(pos % kPageRows);
-  const bool is_v = g >= a.c.Hkv;
-  const int head = is_v ? g - a.c.Hkv : g;
-  if (is_v) load8((const S*)a.v + row * a.v_stride + (int64_t)head * D + e0, x);
-  else rotated((const S*)a.k + row * a.k_stride + (int64_t)head * D, e0, a.rot, a.neighbours, cs, x);
-  char* const at = (char*)(is_v ? a.c.v : a.c.k) + ((int64_t)page * a.c.Hkv + head) * page_bytes(D, CODED ? YOCO_INT4 : YOCO_BF16);
-  if (!CODED) {
-    if (!is_v) {
-      store8((bf16_t*)at + k16_at(r, e0, D), x);
+  __syncthreads();
+
+  const int64_t col = at / kPageRows;
+  int page = -1;                                                                  // at is a multiple of 16: all of its rows are on the page, or none
+  if (at >= 0 && col < a.cols) page = a.table[(int64_t)b * a.cols + col];
+  if (page >= a.c.n_pages) page = -1;
+  const int base = (int)(at & (kPageRows - 1));
+  auto place = [&](void* plane, int head) { return (char*)plane + ((int64_t)page * a.c.Hkv + head) * page_bytes(D, CODED ? YOCO_INT4 : YOCO_BF16); };
+  // the scales of a row's groups, from the pieces of all of its threads
+  auto scales = [&](const float(&x)[8], const float(&y)[8], int e0, int e1, unsigned(&param)[kGroups]) {
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      Group group;
+      if (kGroups == 1 || e0 / 64 == g) group.see(x);
+      if (kGroups == 1 || e1 / 64 == g) group.see(y);
+      group.template join<kThreads>();
+      param[g] = group.param();
+    }
+  };
+  auto of = [&](const unsigned(&param)[kGroups], int e) { return kGroups > 1 && e >= 64 ? param[kGroups - 1] : param[0]; };
+  // V of row r of the page's 16, into the page or, of all 16, into LDS in the page's order: 4 rows side by side
+  auto put_v = [&](int h, int r, const float(&x)[8], const float(&y)[8]) {
+    char* const to = place(a.c.v, h);
+    unsigned char* const lds = turn[slot / kTileRows];
+    const int quad = r / 4 * 16, i4 = r % 4;
+    if constexpr (CODED) {
+      unsigned param[kGroups];
+      scales(x, y, v0, v1, param);
+      const unsigned lo = code8(x, of(param, v0)), hi = code8(y, of(param, v1));
+      if (th < kGroups) *(unsigned*)(to + param4_byte(base + r, th * 64, D)) = of(param, th * 64);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const unsigned char byte = (unsigned char)(((lo >> (4 * j)) & 15u) | (((hi >> (4 * j)) & 15u) << 4));
+        if (whole) lds[(v0 / 32 * 64 + quad + v0 % 16 + j) * 4 + i4] = byte;
+        else to[v4_byte(base + r, v0 + j)] = (char)byte;
+      }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) ((bf16_t*)at)[v16_at(r, e0 + j)] = f32_to_bf16(x[j]);
+      for (int j = 0; j < 8; ++j) {
+        const bf16_t p = f32_to_bf16(x[j]), q = f32_to_bf16(y[j]);
+        if (whole) {
+          ((bf16_t*)lds)[(v0 / 16 * 64 + quad + v0 % 16 + j) * 4 + i4] = p;
+          ((bf16_t*)lds)[(v1 / 16 * 64 + quad + v1 % 16 + j) * 4 + i4] = q;
+        } else {
+          ((bf16_t*)to)[v16_at(base + r, v0 + j)] = p;
+          ((bf16_t*)to)[v16_at(base + r, v1 + j)] = q;
+        }
+      }
     }
-    return;
-  }
-  unsigned param;
-  const unsigned codes = code8(x, param);
-  if (!is_v) {
-    *(unsigned*)(at + k4_byte(r, e0, D)) = codes;
-  } else {
-    const unsigned other = __shfl_xor(codes, 2);                                    // 16 dimensions further on, or back
-    if (e0 / 16 % 2 == 0) {
+  };
+
+  for (; i < last1 * nr; i += kSlots) {
+    const int h = i / nr, r = r0 + i - h * nr;
+    float nx[8], ny[8];
+    if (i + kSlots < last1 * nr) fetch(i + kSlots, nx, ny);
+    if (h < values) rotate(x, y, c0, c1, a.rot, a.neighbours, cs[r]);
+    if (h < keys) {
+      S* const to = (S*)a.q_out + (row_of(r) * a.Hq + h) * D;
+      store8(to + c0, x);
+      store8(to + c1, y);
+    } else if (page >= 0 && t0 + r < n) {
+      if (h >= values) {
+        put_v(h - values, r, x, y);
+      } else {
+        char* const to = place(a.c.k, h - keys);
+        if constexpr (CODED) {
+          unsigned param[kGroups];
+          scales(x, y, c0, c1, param);
+          *(unsigned*)(to + k4_byte(base + r, c0, D)) = code8(x, of(param, c0));
+          *(unsigned*)(to + k4_byte(base + r, c1, D)) = code8(y, of(param, c1));
+          if (th < kGroups) *(unsigned*)(to + param4_byte(base + r, th * 64, D)) = of(param, th * 64);
+        } else {
+          store8((bf16_t*)to + k16_at(base + r, c0, D), x);
+          store8((bf16_t*)to + k16_at(base + r, c1, D), y);
+        }
+      }
+    }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) at[v4_byte(r, e0 + j)] = (char)(((codes >> (4 * j)) & 15u) | (((other >> (4 * j)) & 15u) << 4));
+    for (int j = 0; j < 8; ++j) {
+      x[j] = nx[j];
+      y[j] = ny[j];
     }
   }
-  if (e0 % kCodeGroup == 0) *(unsigned*)(at + param4_byte(r, e0, D)) = param;
+  if (!whole || page < 0) return;
+  int h0 = first > values ? first - values : 0;
+  auto fetch_v = [&](int h0) {
+    if (h0 + slot / kTileRows < last - values) fetch((values + h0 + slot / kTileRows) * kTileRows + slot % kTileRows, x, y);
+  };
+  fetch_v(h0);
+  for (; h0 < last - values; h0 += kSlots / kTileRows) {
+    if (h0 + slot / kTileRows < last - values) put_v(h0 + slot / kTileRows, slot % kTileRows, x, y);
+    fetch_v(h0 + kSlots / kTileRows);
+    __syncthreads();
+    const int left = last - values - h0, some = left < kSlots / kTileRows ? left : kSlots / kTileRows;
+    if constexpr (CODED) {
+      for (int k = threadIdx.x; k < some * (kPlane / 4); k += 256) {
+        const int g = k / (kPlane / 4), u = k % (kPlane / 4);
+        *(unsigned*)(place(a.c.v, h0 + g) + u * 16 + base / 16 * 4) = ((const unsigned*)turn[g])[u];
+      }
+    } else {
+      for (int k = threadIdx.x; k < some * (kPlane / 8); k += 256) {
+        const int g = k / (kPlane / 8), u = k % (kPlane / 8);                     // u: 64 (e / 16) + lane
+        *(uint64_t*)((bf16_t*)place(a.c.v, h0 + g) + ((u / 64 * 2 + base / 32) * 64 + u % 64) * 8 + base / 16 % 2 * 4) = ((const uint64_t*)turn[g])[u];
+      }
+    }
+    __syncthreads();
+  }
 }
 
 // The value that a code stands for.
@@ -176,48 +296,76 @@ __device__ __forceinline__ float decoded(unsigned code, unsigned param) {
   return fmaf((float)code, __uint_as_float(param << 16), __uint_as_float(param & 0xffff0000u));
 }
 
-// 8 dimensions of a row and head a thread; z: K or V.
-template <typename S>
-__global__ void __launch_bounds__(256) read_kernel(yoco_paged_cache c, const int32_t* __restrict__ table, int B, int cols, const int64_t* __restrict__ pos0, int64_t T,
-                                                   S* __restrict__ k, S* __restrict__ v) {
-  const int threads = c.d / 8;
-  const int64_t unit = (int64_t)blockIdx.x * (256 / threads) + threadIdx.x / threads;            // row and head
-  if (unit >= (int64_t)B * T * c.Hkv) return;
-  const int64_t row = unit / c.Hkv;
-  const int head = (int)(unit - row * c.Hkv), b = (int)(row / T), e0 = threadIdx.x % threads * 8;
-  const int64_t pos = pos0[b] + (row - (int64_t)b * T);
-  const bool is_v = blockIdx.y;
-  float x[8] = {};
-  const int page = pos >= 0 && pos < (int64_t)cols * kPageRows ? table[(int64_t)b * cols + pos / kPageRows] : -1;
-  if (page >= 0 && page < c.n_pages) {
-    const int r = (int)(pos % kPageRows);
-    const char* const at = (const char*)(is_v ? c.v : c.k) + ((int64_t)page * c.Hkv + head) * page_bytes(c.d, c.dtype);
-    if (c.dtype == YOCO_INT4) {
-      const unsigned param = *(const unsigned*)(at + param4_byte(r, e0, c.d));
-      if (!is_v) {
-        const unsigned codes = *(const unsigned*)(at + k4_byte(r, e0, c.d));
+// The 16 rows of a page that lie together, of a head and plane: 8 dimensions of a row a thread. V is turned in LDS.
+template <typename S, int D, bool CODED>
+__global__ void __launch_bounds__(256) read_kernel(yoco_paged_cache c, const int32_t* __restrict__ table, int cols, const int64_t* __restrict__ pos0, int64_t T, int tiles, S* __restrict__ k,
+                                                   S* __restrict__ v) {
+  constexpr int kPieces = D / 8;                                                   // of 8 dimensions
+  __shared__ __attribute__((aligned(16))) unsigned short turn[kTileRows][D + 8];
+  const int group = tile_of(blockIdx.x, gridDim.x), b = group / tiles, tile = group - b * tiles, head = blockIdx.y;
+  const bool is_v = blockIdx.z;
+  const int64_t first = pos0[b], at = (first & ~(int64_t)(kTileRows - 1)) + (int64_t)tile * kTileRows;
+  const int t0 = (int)(at - first);
+  const int64_t col = at / kPageRows;
+  const int page = at >= 0 && col < cols ? table[(int64_t)b * cols + col] : -1;
+  const bool there = page >= 0 && page < c.n_pages;
+  const int base = (int)(at & (kPageRows - 1));
+  const char* const from = (const char*)(is_v ? c.v : c.k) + ((int64_t)(there ? page : 0) * c.Hkv + head) * page_bytes(D, CODED ? YOCO_INT4 : YOCO_BF16);
+  if (is_v && there) {
+    if constexpr (CODED) {
+      for (int u = threadIdx.x; u < D * 2; u += 256) {                             // u: 64 (e / 32) + lane; bytes of 4 rows
+        const unsigned w = *(const unsigned*)(from + u * 16 + base / 16 * 4);
+        const int e = u / 64 * 32 + u % 16, r = u % 64 / 16 * 4;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = decoded((codes >> (4 * j)) & 15u, param);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = decoded(((unsigned)(unsigned char)at[v4_byte(r, e0 + j)] >> (e0 / 16 % 2 * 4)) & 15u, param);
+        for (int i = 0; i < 4; ++i) {
+          turn[r + i][e] = (w >> (8 * i)) & 15u;
+          turn[r + i][e + 16] = (w >> (8 * i + 4)) & 15u;
+        }
       }
-    } else if (!is_v) {
-      load8((const bf16_t*)at + k16_at(r, e0, c.d), x);
     } else {
+      for (int u = threadIdx.x; u < D * 4; u += 256) {
+        const uint64_t w = *(const uint64_t*)((const bf16_t*)from + ((u / 64 * 2 + base / 32) * 64 + u % 64) * 8 + base / 16 % 2 * 4);
+        const int e = u / 64 * 16 + u % 16, r = u % 64 / 16 * 4;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = bf16_to_f32(((const bf16_t*)at)[v16_at(r, e0 + j)]);
+        for (int i = 0; i < 4; ++i) turn[r + i][e] = (unsigned short)(w >> (16 * i));
+      }
     }
   }
-  store8((is_v ? v : k) + unit * c.d + e0, x);
+  __syncthreads();
+  const int r = threadIdx.x / kPieces, e0 = threadIdx.x % kPieces * 8;
+  if (r >= kTileRows || t0 + r < 0 || t0 + r >= T) return;
+  float x[8] = {};
+  if (there) {
+    if constexpr (CODED) {
+      const unsigned param = *(const unsigned*)(from + param4_byte(base + r, e0, D)), codes = is_v ? 0u : *(const unsigned*)(from + k4_byte(base + r, e0, D));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = decoded(is_v ? turn[r][e0 + j] : (codes >> (4 * j)) & 15u, param);
+    } else if (is_v) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = bf16_to_f32(turn[r][e0 + j]);
+    } else {
+      load8((const bf16_t*)from + k16_at(base + r, e0, D), x);
+    }
+  }
+  store8((is_v ? v : k) + (((int64_t)b * T + t0 + r) * c.Hkv + head) * D + e0, x);
 }
 
 }  // namespace
 
+namespace {
+// Groups of 16 positions that T rows from any position on can touch.
+int tiles_of(int64_t T) { return (int)((T + 2 * kTileRows - 2) / kTileRows); }
+}  // namespace
+
 hipError_t launch_paged_append(const AppendView& a, int src_dtype, hipStream_t s) {
-  const int heads = 2048 / a.c.d;
-  const dim3 grid((unsigned)(a.B * a.T), (unsigned)((a.Hq + 2 * a.c.Hkv + heads - 1) / heads)), block(256);
-  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
+  const int tiles = tiles_of(a.T), heads = a.Hq + 2 * a.c.Hkv, slots = 4096 / a.c.d;
+  const int64_t groups = (int64_t)a.B * tiles;
+  // Enough workgroups for the chip; of a row or two 8 heads each, so that none does one kind of head after another (a step of 16 rows of 24:8 heads
+  // with 20 heads each 7.0 us).
+  const int64_t rows = a.T < kTileRows ? a.T : kTileRows, useful = rows * 8 > slots ? (heads * rows + slots - 1) / slots : (heads + 7) / 8, wanted = (2048 + groups - 1) / groups;
+  const int parts = (int)(wanted < useful ? wanted : useful), share = (heads + parts - 1) / parts;
+  const dim3 grid((unsigned)groups, (unsigned)((heads + share - 1) / share)), block(256);
+  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, tiles, share); };
   const bool coded = a.c.dtype == YOCO_INT4;
   if (src_dtype == YOCO_F32) {
     if (a.c.d == 128) coded ? go(&append_kernel<float, 128, true>) : go(&append_kernel<float, 128, false>);
@@ -231,10 +379,19 @@ hipError_t launch_paged_append(const AppendView& a, int src_dtype, hipStream_t s
 
 hipError_t launch_paged_read(const yoco_paged_cache& c, const int32_t* table, int B, int cols, const int64_t* pos, int64_t T, void* k, void* v, int dst_dtype,
                              hipStream_t s) {
-  const int64_t units = (int64_t)B * T * c.Hkv, each = 2048 / c.d;
-  const dim3 grid((unsigned)((units + each - 1) / each), 2), block(256);
-  if (dst_dtype == YOCO_F32) hipLaunchKernelGGL(read_kernel<float>, grid, block, 0, s, c, table, B, cols, pos, T, (float*)k, (float*)v);
-  else hipLaunchKernelGGL(read_kernel<bf16_t>, grid, block, 0, s, c, table, B, cols, pos, T, (bf16_t*)k, (bf16_t*)v);
+  const int tiles = tiles_of(T);
+  const dim3 grid((unsigned)((int64_t)B * tiles), c.Hkv, 2), block(256);
+  const bool coded = c.dtype == YOCO_INT4;
+  auto go = [&](auto* kernel, auto* to, auto* to2) { hipLaunchKernelGGL(kernel, grid, block, 0, s, c, table, cols, pos, T, tiles, to, to2); };
+  if (dst_dtype == YOCO_F32) {
+    float *const x = (float*)k, *const y = (float*)v;
+    if (c.d == 128) coded ? go(&read_kernel<float, 128, true>, x, y) : go(&read_kernel<float, 128, false>, x, y);
+    else coded ? go(&read_kernel<float, 64, true>, x, y) : go(&read_kernel<float, 64, false>, x, y);
+  } else {
+    bf16_t *const x = (bf16_t*)k, *const y = (bf16_t*)v;
+    if (c.d == 128) coded ? go(&read_kernel<bf16_t, 128, true>, x, y) : go(&read_kernel<bf16_t, 128, false>, x, y);
+    else coded ? go(&read_kernel<bf16_t, 64, true>, x, y) : go(&read_kernel<bf16_t, 64, false>, x, y);
+  }
   return hipGetLastError();
 }
 

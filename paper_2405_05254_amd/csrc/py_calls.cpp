@@ -442,6 +442,20 @@ Workspace scratch(PyObject* given, size_t need, const at::TensorOptions& on, at:
   return w;
 }
 
+PyObject* tuple(std::initializer_list<at::Tensor> tensors) {
+  PyObject* const out = PyTuple_New((Py_ssize_t)tensors.size());
+  Py_ssize_t i = 0;
+  for (const at::Tensor& t : tensors) {
+    PyObject* const x = out ? THPVariable_Wrap(t) : nullptr;
+    if (!x) {
+      Py_XDECREF(out);                   // with what it holds already
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(out, i++, x);
+  }
+  return out;
+}
+
 // cache, table, pos, k, v, rows, q, turns, neighbours, q_out
 PyObject* paged_append(PyObject* const* a) {
   const yoco_paged_cache c = pages(a[0]);
@@ -479,18 +493,20 @@ PyObject* paged_append(PyObject* const* a) {
   return o.defined() ? wrap(o, a[9]) : nothing();
 }
 
-// cache, table, pos, T, k, v
+// cache, table, pos, T, whether bf16 -> (k, v)
 PyObject* paged_read(PyObject* const* a) {
   const yoco_paged_cache c = pages(a[0]);
   const Table t = table(a[1], "table");
   const int64_t* pos = longs(a[2], "pos", t.B);
   const int64_t T = integer(a[3]);
-  const at::Tensor &k = tensor(a[4], "k"), &v = tensor(a[5], "v");
-  if (!is_rows(k, t.B, T, c.Hkv, c.d) || v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type()) fail("k/v must be [B,T,Hkv,d] as the table and the cache are");
-  void *kp = dev(k, "k"), *vp = dev(v, "v");
-  const int dt = dtype_of(k), B = small(t.B, "B"), cols = small(t.cols, "cols");
-  call([&] { return p_yoco_paged_read(&c, t.p, B, cols, pos, T, kp, vp, dt, stream()); });
-  return nothing();
+  const bool bf16 = truth(a[4]);
+  if (T < 0) fail("T must not be negative");
+  const at::TensorOptions on = tensor(a[1], "table").options().dtype(bf16 ? at::kBFloat16 : at::kFloat);
+  const at::Tensor k = at::empty({t.B, T, c.Hkv, c.d}, on), v = at::empty({t.B, T, c.Hkv, c.d}, on);
+  void *kp = k.data_ptr(), *vp = v.data_ptr();
+  const int B = small(t.B, "B"), cols = small(t.cols, "cols");
+  call([&] { return p_yoco_paged_read(&c, t.p, B, cols, pos, T, kp, vp, bf16 ? YOCO_BF16 : YOCO_F32, stream()); });
+  return tuple({k, v});
 }
 
 // cache, table, q, lens, scale, workspace, out
@@ -541,19 +557,7 @@ PyObject* beam_select(PyObject* const* a) {
   call([&] {
     return p_yoco_beam_select(xp, stride, scores, done, eos < 0 ? -1 : (int)eos, B, W, V, dt, (int32_t*)pp, (int32_t*)tp, (float*)bp, (uint8_t*)ep, w.p, w.bytes, stream());
   });
-  PyObject* const out[4] = {THPVariable_Wrap(parent), THPVariable_Wrap(token), THPVariable_Wrap(best), THPVariable_Wrap(ended)};
-  PyObject* tuple = PyTuple_New(4);
-  bool ok = tuple != nullptr;
-  for (PyObject* x : out) ok = ok && x;
-  for (int i = 0; i < 4; ++i) {
-    if (ok) PyTuple_SET_ITEM(tuple, i, out[i]);
-    else Py_XDECREF(out[i]);
-  }
-  if (!ok) {
-    Py_XDECREF(tuple);
-    return nullptr;
-  }
-  return tuple;
+  return tuple({parent, token, best, ended});
 }
 
 // cache, table, home, parent, lens
@@ -624,7 +628,7 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          ENTRY(gret_prefill, 13),
                          ENTRY(gret_decode, 10),
                          ENTRY(paged_append, 10),
-                         ENTRY(paged_read, 6),
+                         ENTRY(paged_read, 5),
                          ENTRY(paged_attn, 7),
                          ENTRY(beam_select, 5),
                          ENTRY(beam_reorder_pages, 5),
