@@ -4,6 +4,8 @@
 // Selection. Within a beam score + logit - log-sum-exp grows with the logit, so a beam's W best logits are all that can be
 // chosen of it: one pass over the logits keeps, of every chunk, the maximum, the sum of exponentials and the W best, and what
 // is left is small. Candidates of a beam are ordered by logit and then token, candidates of a request by score and then beam.
+#include <limits.h>
+
 #include "decode_tail.h"
 #include "paged.h"
 
@@ -25,40 +27,68 @@ __device__ __forceinline__ float unordered(unsigned u) { return __uint_as_float(
 __device__ __forceinline__ uint64_t key_of(float x, int token) { return (uint64_t)ordered(x) << 32 | (unsigned)~token; }
 constexpr uint64_t kNoKey = 0;            // below every candidate: no logit has these bits but a NaN
 
-__device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane) {
-  return (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)k, lane);
-}
-
-// The W best of a wavefront's keys, N a lane, best first, into `best`; kNoKey where there are fewer. `list` holds W * N keys. Every lane's best
-// one is ranked among the 64: the W-th of those bounds the W-th of all from below, and only W lanes can hold any above it.
-template <int N>
-__device__ __forceinline__ void wave_best(const uint64_t (&k)[N], int W, uint64_t* list, uint64_t* best) {
+// Of the n keys in `list` (LDS of this wavefront) the W best, best first, into `best`; kNoKey where there are fewer.
+__device__ __forceinline__ void rank_keys(const uint64_t* list, int n, int W, uint64_t* best) {
   const int lane = threadIdx.x & 63;
-  uint64_t mine = k[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) mine = k[i] > mine ? k[i] : mine;
-  int rank = 0;
-  for (int j = 0; j < 64; ++j) {
-    const uint64_t other = lane_key(mine, j);
-    rank += other > mine || (other == mine && j < lane);
-  }
-  const uint64_t least = lane_key(mine, __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == W - 1)));
-  int n = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint64_t in = __builtin_amdgcn_ballot_w64(k[i] >= least && k[i] != kNoKey);
-    if (k[i] >= least && k[i] != kNoKey) list[n + __builtin_amdgcn_mbcnt_hi((unsigned)(in >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in, 0))] = k[i];
-    n += __builtin_popcountll(in);
-  }
   if (lane < W) best[lane] = kNoKey;
   __builtin_amdgcn_wave_barrier();
   for (int i = lane; i < n; i += 64) {
     const uint64_t key = list[i];
     int r = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) r += list[j] > key;
     if (r < W) best[r] = key;
   }
   __builtin_amdgcn_wave_barrier();
+}
+// The W best of a wavefront's logits, N a lane (-inf: none), of which logit i of a lane has token(i), into `best`; `mine` is the lane's
+// largest. Every lane's is ranked among the 64: the W-th bounds the W-th of all from below, and few are above it. Of equal ones there may be
+// more than the list holds; then the best are taken out one after another.
+template <int N, typename Token>
+__device__ __forceinline__ void wave_best(float (&x)[N], float mine, int W, uint64_t* list, int room, uint64_t* best, Token token) {
+  int rank = 0;
+#pragma unroll 8
+  for (int j = 0; j < 64; ++j) rank += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), j)) > mine;
+  // the W-th of the lanes' best ones: the least of those that fewer than W are larger than
+  const float least = fmaxf(-over64<LaneMax>(rank < W ? -mine : -INFINITY), -3.402823466e38f);
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint64_t in = __builtin_amdgcn_ballot_w64(x[i] >= least);
+    if (!in) continue;
+    const int at = n + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(in >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in, 0));
+    if (x[i] >= least && at < room) list[at] = key_of(x[i], token(i));
+    n += __builtin_popcountll(in);
+  }
+  if (n <= room) {
+    rank_keys(list, n, W, best);
+    return;
+  }
+  const int lane = threadIdx.x & 63;
+  if (lane < W) best[lane] = kNoKey;
+  __builtin_amdgcn_wave_barrier();
+  for (int r = 0; r < W; ++r) {
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+    m = over64<LaneMax>(m);
+    if (m == -INFINITY) break;
+    int t = INT_MAX;
+#pragma unroll
+    for (int i = 0; i < N; ++i) t = x[i] == m && token(i) < t ? token(i) : t;
+    t = INT_MAX - lanes_max(INT_MAX - t);
+    if (lane == 0) best[r] = key_of(m, t);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = x[i] == m && token(i) == t ? -INFINITY : x[i];
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A NaN becomes -infinity, as no candidate has it, and infinity the largest number.
+__device__ __forceinline__ float in_range(float x) {
+  float z;
+  asm("v_med3_f32 %0, %1, %2, %3" : "=v"(z) : "v"(x), "v"(-INFINITY), "v"(3.402823466e38f));   // of a NaN: the least of the others
+  return z;
 }
 
 // 8 logits from element `at` on, those outside [lo, hi) as -inf. `at` is a multiple of 8 and `end` the number of elements that there are.
@@ -93,51 +123,57 @@ __device__ __forceinline__ float sum_exp(float m, float from, float sum) {      
   return from == -INFINITY ? 0.f : sum * __expf(from - m);
 }
 
-// What a chunk leaves: maximum and sum of exponentials (two floats), then its W best keys.
+// What a chunk leaves: maximum and sum of exponentials (two floats) and its W best keys.
 __host__ __device__ inline size_t chunk_words(int W) { return 1 + (size_t)W; }     // of 64 bits
+
+constexpr int kMaxChunks = 65;            // a row that starts inside a piece of 8 reaches into one chunk more than 64
+constexpr int kListKeys = 128;
 
 template <typename S, int VECS>           // 8-logit pieces a thread
 __global__ void __launch_bounds__(256) select_chunks_kernel(SelectView a, uint64_t* ws) {
-  __shared__ uint64_t list[4][kMaxBeams * VECS * 8], best[4][kMaxBeams];
+  __shared__ uint64_t list[4][kListKeys], best[4 * kMaxBeams], joined[kMaxBeams];
   __shared__ float stats[4][2];
   const int row = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, W = a.W;
-  if (a.done && a.done[row]) return;
+  if (a.done && a.done[row]) return;                 // a finished beam's logits are not read
   const int64_t first = (int64_t)row * a.stride, last = first + a.V, end = (int64_t)(a.B * W - 1) * a.stride + a.V;
   const int64_t v0 = first / 8 + (int64_t)blockIdx.x * (VECS * 256) + threadIdx.x;
-  uint64_t k[VECS * 8];
   float m = -INFINITY, l = 0.f, x[VECS * 8];
 #pragma unroll
   for (int i = 0; i < VECS; ++i) {
     const int64_t at = (v0 + i * 256) * 8;
-    float y[8] = {};
-    if (at < last) logits8((const S*)a.logits, at, end, y);
+    float y[8] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (at < last) {
+      logits8((const S*)a.logits, at, end, y);
+      if (at < first || at + 8 > last) {             // the ends of the row lie inside
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      // a NaN is no candidate, and an infinity the largest number
-      const bool in = at + j >= first && at + j < last && !is_nan(y[j]) && y[j] != -INFINITY;
-      const float z = in ? fminf(y[j], 3.402823466e38f) : -INFINITY;
-      x[i * 8 + j] = z;
-      m = fmaxf(m, z);
-      k[i * 8 + j] = in ? key_of(z, (int)(at + j - first)) : kNoKey;
+        for (int j = 0; j < 8; ++j) y[j] = at + j >= first && at + j < last ? y[j] : -INFINITY;
+      }
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[i * 8 + j] = y[j];
   }
+#pragma unroll
+  for (int i = 0; i < VECS * 8; ++i) {
+    x[i] = in_range(x[i]);
+    m = fmaxf(m, x[i]);
+  }
+  const float mine = m;
   m = over64<LaneMax>(m);
   if (m > -INFINITY) {
 #pragma unroll
     for (int i = 0; i < VECS * 8; ++i) l += __expf(x[i] - m);
   }
   l = over64<LaneSum>(l);
-  wave_best(k, W, list[wave], best[wave]);
+  wave_best(x, mine, W, list[wave], kListKeys, best + wave * W, [&](int i) { return (int)((v0 + i / 8 * 256) * 8 + i % 8 - first); });
   if (lane == 0) {
     stats[wave][0] = m;
     stats[wave][1] = l;
   }
   __syncthreads();
-  if (wave) return;
+  if (wave > 0) return;
+  rank_keys(best, 4 * W, W, joined);
   uint64_t* const out = ws + ((size_t)row * gridDim.x + blockIdx.x) * chunk_words(W);
-  const uint64_t mine[1] = {lane < 4 * W ? best[lane / W][lane % W] : kNoKey};
-  wave_best(mine, W, list[0], best[0]);
-  if (lane < W) out[1 + lane] = best[0][lane];
+  if (lane < W) out[1 + lane] = joined[lane];
   if (lane == 0) {
     const float M = fmaxf(fmaxf(stats[0][0], stats[1][0]), fmaxf(stats[2][0], stats[3][0]));
     float sum = 0.f;
@@ -146,39 +182,41 @@ __global__ void __launch_bounds__(256) select_chunks_kernel(SelectView a, uint64
   }
 }
 
-constexpr int kMaxChunks = 65;            // a row that starts inside a piece of 8 reaches into one chunk more than 64
-constexpr int kMergeKeys = (kMaxChunks * kMaxBeams + 63) / 64;
-
-// A request's candidates from those of its beams' chunks.
-__global__ void __launch_bounds__(256) select_merge_kernel(SelectView a, const uint64_t* ws, int chunks) {
-  __shared__ uint64_t list[4][kMaxBeams * kMergeKeys], best[kMaxBeams][kMaxBeams];
+// A request's continuations from what its chunks have left: a wavefront a beam, KEYS of its chunks' keys a lane, then a candidate a thread.
+template <int KEYS>
+__global__ void __launch_bounds__(64 * kMaxBeams) select_merge_kernel(SelectView a, const uint64_t* ws, int chunks) {
+  __shared__ uint64_t list[kMaxBeams][kListKeys], best[kMaxBeams][kMaxBeams];
   __shared__ float lse[kMaxBeams], score[kMaxBeams * kMaxBeams];
   const int b = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, W = a.W;
-  for (int w = wave; w < W; w += 4) {
-    const int row = b * W + w;
-    if (a.done && a.done[row]) continue;
-    const uint64_t* const p = ws + (size_t)row * chunks * chunk_words(W);
-    float m = -INFINITY, l = 0.f;
-    for (int c = lane; c < chunks; c += 64) {
-      const uint64_t x = p[c * chunk_words(W)];
-      const float mc = __uint_as_float((unsigned)x), M = fmaxf(m, mc);
-      l = sum_exp(M, m, l) + sum_exp(M, mc, __uint_as_float((unsigned)(x >> 32)));
-      m = M;
-    }
-    const float M = over64<LaneMax>(m);
-    l = over64<LaneSum>(sum_exp(M, m, l));
-    uint64_t k[kMergeKeys];
+  if (!(a.done && a.done[b * W + wave])) {
+    const uint64_t* const p = ws + (size_t)(b * W + wave) * chunks * chunk_words(W);
+    constexpr int kStats = (kMaxChunks + 63) / 64;
+    uint64_t stats[kStats], keys[KEYS];
 #pragma unroll
-    for (int i = 0; i < kMergeKeys; ++i) {
+    for (int i = 0; i < kStats; ++i) stats[i] = i * 64 + lane < chunks ? p[(size_t)(i * 64 + lane) * chunk_words(W)] : 0xff800000ull;      // -inf, 0
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) {
       const int j = i * 64 + lane, c = j / W;
-      k[i] = c < chunks ? p[c * chunk_words(W) + 1 + j % W] : kNoKey;
+      keys[i] = c < chunks ? p[c * chunk_words(W) + 1 + (j - c * W)] : kNoKey;
     }
-    wave_best(k, W, list[wave], best[w]);
-    if (lane == 0) lse[w] = M + logf(l);
+    float m = -INFINITY, l = 0.f, x[KEYS], most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kStats; ++i) m = fmaxf(m, __uint_as_float((unsigned)stats[i]));
+    m = over64<LaneMax>(m);
+#pragma unroll
+    for (int i = 0; i < kStats; ++i) l += sum_exp(m, __uint_as_float((unsigned)stats[i]), __uint_as_float((unsigned)(stats[i] >> 32)));
+    l = over64<LaneSum>(l);
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) {
+      x[i] = keys[i] == kNoKey ? -INFINITY : unordered((unsigned)(keys[i] >> 32));
+      most = fmaxf(most, x[i]);
+    }
+    wave_best(x, most, W, list[wave], kListKeys, best[wave], [&](int i) { return (int)~(unsigned)keys[i]; });
+    if (lane == 0) lse[wave] = m + logf(l);
   }
   __syncthreads();
   // a candidate a thread, in the order that decides between equal scores
-  const int t = threadIdx.x, w = t / W, r = t % W;
+  const int t = threadIdx.x, w = t / W, r = t - w * W;
   float mine = -INFINITY;
   int token = a.eos >= 0 ? a.eos : 0;
   if (w < W) {
@@ -195,6 +233,7 @@ __global__ void __launch_bounds__(256) select_merge_kernel(SelectView a, const u
   __syncthreads();
   if (w >= W) return;
   int rank = 0;
+#pragma unroll 4
   for (int j = 0; j < W * W; ++j) rank += score[j] > mine || (score[j] == mine && j < t);
   if (rank >= W) return;
   const int out = b * W + rank;
@@ -305,13 +344,19 @@ size_t beam_select_workspace(int B, int W, int V) { return (size_t)B * W * selec
 
 hipError_t launch_beam_select(const SelectView& a, int dtype, void* workspace, hipStream_t s) {
   const int rows = a.B * a.W, vecs = select_pieces(rows, a.V), chunks = select_chunks(vecs, a.V);
+  uint64_t* const ws = (uint64_t*)workspace;
   const dim3 grid(chunks, rows), block(256);
-  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, (uint64_t*)workspace); };
+  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, ws); };
   if (dtype == YOCO_F32) vecs == 1 ? go(&select_chunks_kernel<float, 1>) : vecs == 2 ? go(&select_chunks_kernel<float, 2>) : go(&select_chunks_kernel<float, 4>);
   else vecs == 1 ? go(&select_chunks_kernel<bf16_t, 1>) : vecs == 2 ? go(&select_chunks_kernel<bf16_t, 2>) : go(&select_chunks_kernel<bf16_t, 4>);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(select_merge_kernel, dim3(a.B), block, 0, s, a, (const uint64_t*)workspace, chunks);
+  if (const hipError_t e = hipGetLastError()) return e;
+  const int keys = (chunks * a.W + 63) / 64;         // a lane's, at most 17
+  auto merge = [&](auto* kernel) { hipLaunchKernelGGL(kernel, dim3(a.B), dim3(64 * a.W), 0, s, a, (const uint64_t*)ws, chunks); };
+  if (keys <= 1) merge(&select_merge_kernel<1>);
+  else if (keys <= 2) merge(&select_merge_kernel<2>);
+  else if (keys <= 4) merge(&select_merge_kernel<4>);
+  else if (keys <= 8) merge(&select_merge_kernel<8>);
+  else merge(&select_merge_kernel<(kMaxChunks * kMaxBeams + 63) / 64>);
   return hipGetLastError();
 }
 
