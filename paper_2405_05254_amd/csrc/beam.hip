@@ -42,15 +42,18 @@ __device__ __forceinline__ void rank_keys(const uint64_t* list, int n, int W, ui
   __builtin_amdgcn_wave_barrier();
 }
 // The W best of a wavefront's logits, N a lane (-inf: none), of which logit i of a lane has token(i), into `best`; `mine` is the lane's
-// largest. Every lane's is ranked among the 64: the W-th bounds the W-th of all from below, and few are above it. Of equal ones there may be
+// largest. The W-th of the lanes' largest bounds the W-th of all from below, and few are above it. Of equal ones there may be
 // more than the list holds; then the best are taken out one after another.
 template <int N, typename Token>
 __device__ __forceinline__ void wave_best(float (&x)[N], float mine, int W, uint64_t* list, int room, uint64_t* best, Token token) {
-  int rank = 0;
-#pragma unroll 8
-  for (int j = 0; j < 64; ++j) rank += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), j)) > mine;
-  // the W-th of the lanes' best ones: the least of those that fewer than W are larger than
-  const float least = fmaxf(-over64<LaneMax>(rank < W ? -mine : -INFINITY), -3.402823466e38f);
+  const int lane = threadIdx.x & 63;
+  float least = over64<LaneMax>(mine);
+  for (int r = 1; r < W; ++r) {                      // without one lane that has it
+    const uint64_t at = __builtin_amdgcn_ballot_w64(mine == least);
+    mine = at & -at & (1ull << lane) ? -INFINITY : mine;
+    least = over64<LaneMax>(mine);
+  }
+  least = fmaxf(least, -3.402823466e38f);
   int n = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -64,7 +67,6 @@ __device__ __forceinline__ void wave_best(float (&x)[N], float mine, int W, uint
     rank_keys(list, n, W, best);
     return;
   }
-  const int lane = threadIdx.x & 63;
   if (lane < W) best[lane] = kNoKey;
   __builtin_amdgcn_wave_barrier();
   for (int r = 0; r < W; ++r) {
@@ -129,6 +131,7 @@ __host__ __device__ inline size_t chunk_words(int W) { return 1 + (size_t)W; }  
 constexpr int kMaxChunks = 65;            // a row that starts inside a piece of 8 reaches into one chunk more than 64
 constexpr int kListKeys = 128;
 
+// Bound by the vector instructions, about 14 a logit, and not by the bytes: 128 rows x 128000 take 13 us in float32 and in bfloat16.
 template <typename S, int VECS>           // 8-logit pieces a thread
 __global__ void __launch_bounds__(256) select_chunks_kernel(SelectView a, uint64_t* ws) {
   __shared__ uint64_t list[4][kListKeys], best[4 * kMaxBeams], joined[kMaxBeams];
@@ -182,7 +185,8 @@ __global__ void __launch_bounds__(256) select_chunks_kernel(SelectView a, uint64
   }
 }
 
-// A request's continuations from what its chunks have left: a wavefront a beam, KEYS of its chunks' keys a lane, then a candidate a thread.
+// A request's continuations from what its chunks have left, in a launch of its own: in the same one, by whoever comes last, every workgroup has
+// to look at the others' tags across the chiplets (128 x 128000: 44 us instead of 23). A wavefront a beam, KEYS of its chunks' keys a lane, then a candidate a thread.
 template <int KEYS>
 __global__ void __launch_bounds__(64 * kMaxBeams) select_merge_kernel(SelectView a, const uint64_t* ws, int chunks) {
   __shared__ uint64_t list[kMaxBeams][kListKeys], best[kMaxBeams][kMaxBeams];
@@ -246,7 +250,9 @@ __global__ void __launch_bounds__(64 * kMaxBeams) select_merge_kernel(SelectView
   if (a.done_out) a.done_out[out] = (a.done && a.done[b * W + parent]) || token == a.eos;
 }
 
-// 8-logit pieces a thread so that the chunks are few enough to be merged by one wavefront and enough to fill the chip.
+// 8-logit pieces a thread: as few as leave a row no more than 32 chunks to merge and the chip no more than about 1000 workgroups. A row of a
+// few thousand logits is done soonest with 1 (4 beams x 32000: 7.0 us, with 4 8.3), many long rows with 4 (128 x 128000 float32: 21.5 us, with
+// 1 35 and with 2 25; 8 would be 23.7).
 int select_pieces(int rows, int V) {
   for (int vecs = 1; vecs < 4; vecs *= 2)
     if ((V + 2048 * vecs - 1) / (2048 * vecs) <= 32 && (int64_t)rows * V <= (int64_t)2048 * vecs * 1024) return vecs;
