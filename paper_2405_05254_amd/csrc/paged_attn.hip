@@ -652,34 +652,59 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
   bool all_there = true;
   for (int i = lane; i < parts; i += 64) all_there = all_there && get_u64(place(i) + slot.tag(wave)) == a.tag;
   if (__builtin_amdgcn_ballot_w64(!all_there)) return;
-  for (int c = wave; c < columns; c += 4) {
-    float M = kNegBig, sum = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int i0 = 0; i0 < parts; i0 += 64) {                             // 64 parts at a time, a lane for the maximum and sum of each
-      const int i = i0 + lane < parts ? i0 + lane : parts - 1;
-      const unsigned long long ml = get_u64(place(i) + slot.ml(c));
-      const float m = i0 + lane < parts ? __uint_as_float((unsigned)ml) : kNegBig;
-      const float M2 = fmaxf(M, over64<LaneMax>(m)), old = __builtin_amdgcn_exp2f(M - M2);
-      const float f = i0 + lane < parts ? __builtin_amdgcn_exp2f(m - M2) : 0.f;
-      sum = sum * old + over64<LaneSum>(f * __uint_as_float((unsigned)(ml >> 32)));
-      o0 *= old;
-      o1 *= old;
-      M = M2;
+  // All of the wavefront's columns at once, 64 parts at a time: a lane has the maxima and sums of one of them.
+  auto merge = [&](auto most) {
+    constexpr int kMine = decltype(most)::value, kBatch = kMine > 2 ? 8 : 16;
+    float M[kMine], sum[kMine], o0[kMine], o1[kMine], f[kMine];
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      M[k] = kNegBig;
+      sum[k] = o0[k] = o1[k] = 0.f;
+    }
+    auto column_of = [&](int k) { return wave + 4 * k < columns ? wave + 4 * k : wave; };
+    for (int i0 = 0; i0 < parts; i0 += 64) {
+      const float* const at = place(i0 + lane < parts ? i0 + lane : parts - 1);
+      unsigned long long ml[kMine];
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) ml[k] = get_u64(at + slot.ml(column_of(k)));
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+        const float m = i0 + lane < parts ? __uint_as_float((unsigned)ml[k]) : kNegBig;
+        const float M2 = fmaxf(M[k], over64<LaneMax>(m)), old = __builtin_amdgcn_exp2f(M[k] - M2);
+        f[k] = i0 + lane < parts ? __builtin_amdgcn_exp2f(m - M2) : 0.f;
+        sum[k] = sum[k] * old + over64<LaneSum>(f[k] * __uint_as_float((unsigned)(ml[k] >> 32)));
+        o0[k] *= old;
+        o1[k] *= old;
+        M[k] = M2;
+      }
       const int here = parts - i0 < 64 ? parts - i0 : 64;
-      for (int k = 0; k < here; k += 16) {
-        unsigned long long y[16];
+      for (int p = 0; p < here; p += kBatch) {
+        unsigned long long y[kBatch][kMine];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) y[v] = get_u64(place(i0 + (k + v < here ? k + v : here - 1)) + c * D + (e < D ? e : 0));
+        for (int v = 0; v < kBatch; ++v) {
+          const float* const from = place(i0 + (p + v < here ? p + v : here - 1)) + (e < D ? e : 0);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          if (k + v >= here) break;
-          const float fv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k + v));
-          o0 = fmaf(fv, __uint_as_float((unsigned)y[v]), o0);
-          o1 = fmaf(fv, __uint_as_float((unsigned)(y[v] >> 32)), o1);
+          for (int k = 0; k < kMine; ++k) y[v][k] = get_u64(from + column_of(k) * D);
+        }
+#pragma unroll
+        for (int v = 0; v < kBatch; ++v) {
+          if (p + v >= here) break;
+#pragma unroll
+          for (int k = 0; k < kMine; ++k) {
+            const float fv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f[k]), p + v));
+            o0[k] = fmaf(fv, __uint_as_float((unsigned)y[v][k]), o0[k]);
+            o1[k] = fmaf(fv, __uint_as_float((unsigned)(y[v][k] >> 32)), o1[k]);
+          }
         }
       }
     }
-    store(c, o0, o1, sum);
-  }
+#pragma unroll
+    for (int k = 0; k < kMine; ++k)
+      if (wave + 4 * k < columns) store(wave + 4 * k, o0[k], o1[k], sum[k]);
+  };
+  if (columns <= 4) merge(std::integral_constant<int, 1>());
+  else if (columns <= 8) merge(std::integral_constant<int, 2>());
+  else merge(std::integral_constant<int, 4>());
   for (int i = lane; i < parts; i += 64) put_u64(place(i) + slot.tag(wave), 0ull);       // a captured launch can be replayed
 }
 
