@@ -28,8 +28,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegBig = -1.0e30f;      // "no row seen yet": finite, so m - m never makes NaN
-constexpr int kMinPages = 16;            // of a workgroup, where there are more
-constexpr int kManyPages = 32;
+constexpr int kWholePages = 16;          // as many are not worth a merge, ...
+constexpr int kMinPages = 2;             // ... and a wavefront has no fewer
+constexpr int kManyPages = 8;            // of a wavefront
+constexpr int kWavesPlain = 4;
 constexpr int kAhead4 = 2, kAhead2 = 4, kAheadPlain = 8;
 
 // What a workgroup takes: pages [p0, p1) of a sequence, for a KV head (and column tile).
@@ -43,6 +45,7 @@ struct Piece {
 __device__ __forceinline__ int up_to(int x, int by) { return (x + by - 1) / by * by; }
 
 // The pages of a batch, shared out; every workgroup does so alike. Sequences are looked at 64 at a time, one a lane.
+template <int WAVES>
 struct Shares {
   const int64_t* lens;
   int B, cols, heads, units;             // heads: KV heads x column tiles; units: workgroups to share the pages out to
@@ -65,18 +68,18 @@ struct Shares {
     if (B > 64) look(0);
   }
   // Ranges where both a range and a sequence have many pages.
-  __device__ __forceinline__ bool ranges() const { return total / units >= kManyPages && total / (B * heads) >= 2 * kManyPages; }
+  __device__ __forceinline__ bool ranges() const { return total / units >= WAVES * kManyPages && total / (B * heads) >= 64; }
   static __device__ __forceinline__ int scan(int x) {
     return lane_scan(x, [](int a, int b) { return a + b; });
   }
 
   // Few pages: a workgroup has one piece, and pieces end with their sequence, because a second beginning costs as much as many pages.
   __device__ __forceinline__ bool piece(int id, Piece& x) {
-    const int lane = threadIdx.x & 63, grain = 4;
+    const int lane = threadIdx.x & 63, grain = WAVES;
     int share = total / units + 1, each = 0, n = 0, slots = 0;
-    share = share < kMinPages ? kMinPages : up_to(share, grain);
+    share = share < WAVES * kMinPages ? WAVES * kMinPages : up_to(share, grain);
     auto cut = [&] {
-      const int wanted = pages > share ? about_ceil_div(pages, share) : 1;
+      const int wanted = pages > share && pages > kWholePages ? about_ceil_div(pages, share) : 1;
       each = up_to(about_ceil_div(pages + 1, wanted), grain);              // + 1: above 0
       n = pages > each ? about_ceil_div(pages, each) : 1;
     };
@@ -149,7 +152,7 @@ struct Shares {
 template <int D>
 struct Slot {                            // of a partial result: vectors, then (max, sum), then a tag for each wavefront
   int columns;
-  __host__ __device__ size_t floats() const { return (size_t)columns * (D + 2) + 8; }
+  __host__ __device__ size_t floats() const { return (size_t)columns * (D + 2) + 16; }
   __device__ __forceinline__ int ml(int c) const { return columns * D + 2 * c; }
   __device__ __forceinline__ int tag(int wave) const { return columns * (D + 2) + 2 * wave; }
 };
@@ -521,19 +524,19 @@ struct Plain {
 
 __device__ __forceinline__ unsigned pair_bf16(float a, float b) { return (unsigned)f32_to_bf16(a) | ((unsigned)f32_to_bf16(b) << 16); }
 
-template <int D>
+template <int D, int WAVES>
 struct Merge {
-  float o[4][16][D + 4], ml[4][16][2];
+  float o[WAVES][16][D + 4], ml[WAVES][16][2];
 };
 // The states that are merged at the end lie where the scales of the pages were.
-template <int D, typename Form>
+template <int D, int WAVES, typename Form>
 union Lds {
-  char params[4 * Form::kLds];
-  Merge<D> red;
+  char params[WAVES * Form::kLds];
+  Merge<D, WAVES> red;
 };
 
-template <int D, typename Form>
-__device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict__ table, const Piece& piece, Merge<D>& red, char* params) {
+template <int D, int WAVES, typename Form>
+__device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict__ table, const Piece& piece, Merge<D, WAVES>& red, char* params) {
   constexpr int NP = Form::kPages, NC = Form::kColumns;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int n = lane & 15, qg = lane >> 4, bank = n / NC;
@@ -570,11 +573,11 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
   Form::prepare(q, raw, a.scale);
   // A wavefront's pages, 64 at a time: a lane has the entry of the table for one of them. In the loop nothing is loaded under a
   // condition, so that every wait is for the oldest loads alone.
-  for (int p0 = piece.p0 + wave; p0 < p1; p0 += 256) {
-    const int mine = p0 + 4 * lane, id = row[mine < p1 ? mine : p1 - 1], left = len - mine * kPageRows;
+  for (int p0 = piece.p0 + wave; p0 < p1; p0 += 64 * WAVES) {
+    const int mine = p0 + WAVES * lane, id = row[mine < p1 ? mine : p1 - 1], left = len - mine * kPageRows;
     const bool is = mine < p1 && id >= 0 && id < a.c.n_pages;
     const int page = is ? id : 0, has = is ? left < kPageRows ? left : kPageRows : -1;       // -1: no such page
-    const int count = (p1 - p0 + 3) / 4 < 64 ? (p1 - p0 + 3) / 4 : 64;
+    const int count = (p1 - p0 + WAVES - 1) / WAVES < 64 ? (p1 - p0 + WAVES - 1) / WAVES : 64;
     int now[NP], next[NP], rows[NP], nv;
 #pragma unroll
     for (int j = 0; j < NP; ++j) now[j] = __builtin_amdgcn_readlane(page, j);
@@ -583,7 +586,7 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
         rows[j] = __builtin_amdgcn_readlane(has, i + j);
-        if (NP == 1 || bank == j) nv = rows[j] < 0 ? 0 : seen - (p0 + 4 * (i + j)) * kPageRows;
+        if (NP == 1 || bank == j) nv = rows[j] < 0 ? 0 : seen - (p0 + WAVES * (i + j)) * kPageRows;
       }
     };
     int i = 0;
@@ -609,7 +612,7 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
   }
   __syncthreads();
 
-  // A wavefront has every fourth column to itself: it merges the wavefronts' and banks' states, and publishes its part or, where it finds
+  // Column c is wavefront c % WAVES's: it merges the wavefronts' and banks' states, and publishes its part or, where it finds
   // all parts published, merges those.
   const int parts = piece.parts, e = lane * 2;
   auto place = [&](int i) { return a.ws + (size_t)(piece.ranges ? 2 * (piece.slot + i) + (i == 0) : piece.slot + i) * slot.floats(); };
@@ -620,15 +623,15 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
     const float inv = opaque_bits(sum) ? 1.f / sum : 0.f;
     *(unsigned*)(a.o + (((int64_t)b * a.T + t) * a.Hq + g * a.G + (col - t * a.G)) * D + e) = pair_bf16(o0 * inv, o1 * inv);
   };
-  for (int c = wave; c < columns; c += 4) {
+  for (int c = wave; c < columns; c += WAVES) {
     float M = kNegBig;
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
+    for (int w = 0; w < WAVES; ++w)
 #pragma unroll
       for (int j = 0; j < NP; ++j) M = fmaxf(M, red.ml[w][j * NC + c][0]);
     float sum = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
+    for (int w = 0; w < WAVES; ++w)
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
         const float f = __builtin_amdgcn_exp2f(red.ml[w][j * NC + c][0] - M);
@@ -661,7 +664,7 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
       M[k] = kNegBig;
       sum[k] = o0[k] = o1[k] = 0.f;
     }
-    auto column_of = [&](int k) { return wave + 4 * k < columns ? wave + 4 * k : wave; };
+    auto column_of = [&](int k) { return wave + WAVES * k < columns ? wave + WAVES * k : wave; };
     for (int i0 = 0; i0 < parts; i0 += 64) {
       const float* const at = place(i0 + lane < parts ? i0 + lane : parts - 1);
       unsigned long long ml[kMine];
@@ -700,19 +703,19 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
     }
 #pragma unroll
     for (int k = 0; k < kMine; ++k)
-      if (wave + 4 * k < columns) store(wave + 4 * k, o0[k], o1[k], sum[k]);
+      if (wave + WAVES * k < columns) store(wave + WAVES * k, o0[k], o1[k], sum[k]);
   };
-  if (columns <= 4) merge(std::integral_constant<int, 1>());
-  else if (columns <= 8) merge(std::integral_constant<int, 2>());
-  else merge(std::integral_constant<int, 4>());
+  if (columns <= WAVES) merge(std::integral_constant<int, 1>());
+  else if (columns <= 2 * WAVES) merge(std::integral_constant<int, 2>());
+  else merge(std::integral_constant<int, 16 / WAVES>());
   for (int i = lane; i < parts; i += 64) put_u64(place(i) + slot.tag(wave), 0ull);       // a captured launch can be replayed
 }
 
 // Long: the form where a wavefront has many pages.
-template <int D, typename Form, typename Long>
-__global__ void __launch_bounds__(256, 2) attn_kernel(Args a, const int32_t* __restrict__ table) {
-  __shared__ __attribute__((aligned(16))) Lds<D, Long> lds;
-  Shares shares(a.lens, a.B, a.cols, a.c.Hkv * a.tiles, a.units);
+template <int D, int WAVES, typename Form, typename Long>
+__global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(Args a, const int32_t* __restrict__ table) {
+  __shared__ __attribute__((aligned(16))) Lds<D, WAVES, Long> lds;
+  Shares<WAVES> shares(a.lens, a.B, a.cols, a.c.Hkv * a.tiles, a.units);
   const int me = blockIdx.x;
   const bool ranges = shares.ranges();
   Piece piece;
@@ -721,7 +724,7 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(Args a, const int32_t* __r
     const int row = a.T * a.Hq * (D / 2);                                // a sequence without rows is in no range: its outputs are zeros
     for (int b = me; b < a.B; b += gridDim.x)
       if (a.lens[b] <= 0)
-        for (int i = threadIdx.x; i < row; i += 256) ((unsigned*)a.o)[(int64_t)b * row + i] = 0;
+        for (int i = threadIdx.x; i < row; i += 64 * WAVES) ((unsigned*)a.o)[(int64_t)b * row + i] = 0;
     if (me >= a.units) return;
     u = shares.begin(me);
     end = shares.begin(me + 1);
@@ -732,37 +735,56 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(Args a, const int32_t* __r
     if (ranges) piece = shares.piece_at(u, end, before);
     const int pages = piece.p1 - piece.p0;
     u += ranges ? pages : 1;
-    if (!std::is_same<Form, Long>::value && pages >= kManyPages) attend<D, Long>(a, table, piece, lds.red, lds.params);
-    else attend<D, Form>(a, table, piece, lds.red, lds.params);
+    if (!std::is_same<Form, Long>::value && pages >= WAVES * kManyPages) attend<D, WAVES, Long>(a, table, piece, lds.red, lds.params);
+    else attend<D, WAVES, Form>(a, table, piece, lds.red, lds.params);
     __syncthreads();                                                     // what the merge has read is written again
   }
 }
 
-// Workgroups that the pages are shared out to. Rounding a sequence's last piece up makes at most one more for each sequence and head; of those that are
-// cut there are at most twice as many pieces as shares.
-int attn_units(int dtype) { return dtype == YOCO_INT4 ? 2 * compute_units() : compute_units(); }
+// Wavefronts of a workgroup and workgroups that the pages are shared out to, of 4 bits two wavefronts a SIMD in all. With 8 there are half as many
+// parts to merge; with 4 workgroups overlap, and shorter pieces are had. 8 where every piece is part of something longer:
+// 3 x 20000 rows, 24 pairs of sequence and KV head: 17.6 us, with 4 20.5; 64 x 1000, 512 pairs: 19.8, with 4 14.1; 8 x 3000, 64 pairs of few pages: 14.9, with 4 12.2.
+struct Plan {
+  int waves, units;
+};
+Plan attn_plan(int dtype, int64_t segments, int cols) {
+  const int cus = compute_units();
+  if (dtype != YOCO_INT4) return {kWavesPlain, cus};
+  const bool eight = segments * 2 < cus && segments * cols >= 16 * (int64_t)cus;
+  return {eight ? 8 : 4, eight ? cus : 2 * cus};
+}
+int64_t segments_of(const PagedAttnView& a) { return (int64_t)a.B * a.c.Hkv * ((a.T * (a.Hq / a.c.Hkv) + 15) / 16); }
 
 }  // namespace
 
+// Rounding a sequence's last piece up makes at most one more for each sequence and head; of those that are cut there are at most twice as many pieces
+// as shares.
 size_t paged_attn_workspace(const PagedAttnView& a) {
   const int G = a.Hq / a.c.Hkv, columns = a.T * G < 16 ? a.T * G : 16;
   const size_t floats = a.c.d == 128 ? Slot<128>{columns}.floats() : Slot<64>{columns}.floats();
-  return (size_t)2 * attn_units(a.c.dtype) * floats * sizeof(float);
+  return (size_t)2 * attn_plan(a.c.dtype, segments_of(a), a.cols).units * floats * sizeof(float);
 }
 
 hipError_t launch_paged_attn(const PagedAttnView& v, void* workspace, unsigned long long tag, hipStream_t s) {
-  const int G = v.Hq / v.c.Hkv, columns = v.T * G, tiles = (columns + 15) / 16, units = attn_units(v.c.dtype);
-  const Args a = {v.c, (const bf16_t*)v.q, (bf16_t*)v.o, v.lens, (float*)workspace, tag, v.B, v.cols, v.T, v.Hq, G, tiles, units, v.scale};
+  const int G = v.Hq / v.c.Hkv, columns = v.T * G, tiles = (columns + 15) / 16;
+  const int64_t segments = segments_of(v);
+  const Plan plan = attn_plan(v.c.dtype, segments, v.cols);
+  const Args a = {v.c, (const bf16_t*)v.q, (bf16_t*)v.o, v.lens, (float*)workspace, tag, v.B, v.cols, v.T, v.Hq, G, tiles, plan.units, v.scale};
   // no more pieces than pages
-  const int64_t segments = (int64_t)v.B * v.c.Hkv * tiles, most = segments * ((v.cols + kMinPages - 1) / kMinPages);
-  const dim3 grid((unsigned)(segments + units < most ? segments + units : most));
-  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, v.table); };
+  const int64_t most = segments * ((v.cols + plan.waves * kMinPages - 1) / (plan.waves * kMinPages));
+  const dim3 grid((unsigned)(segments + plan.units < most ? segments + plan.units : most));
+  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * plan.waves), 0, s, a, v.table); };
+  auto coded = [&](auto d, auto waves) {
+    constexpr int D = decltype(d)::value, WAVES = decltype(waves)::value;
+    if (columns <= 4) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 4, kAhead4>>);
+    else if (columns <= 8) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 2, kAhead2>>);
+    else go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 1, 2>>);
+  };
   auto by_d = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (v.c.dtype != YOCO_INT4) go(&attn_kernel<D, Plain<D, kAheadPlain>, Plain<D, kAheadPlain>>);
-    else if (columns <= 4) go(&attn_kernel<D, Coded<D, 1, 2>, Coded<D, 4, kAhead4>>);
-    else if (columns <= 8) go(&attn_kernel<D, Coded<D, 1, 2>, Coded<D, 2, kAhead2>>);
-    else go(&attn_kernel<D, Coded<D, 1, 2>, Coded<D, 1, 2>>);
+    if (v.c.dtype != YOCO_INT4) go(&attn_kernel<D, kWavesPlain, Plain<D, kAheadPlain>, Plain<D, kAheadPlain>>);
+    else if (plan.waves == 8) coded(d, std::integral_constant<int, 8>());
+    else coded(d, std::integral_constant<int, 4>());
   };
   if (v.c.d == 128) by_d(std::integral_constant<int, 128>());
   else by_d(std::integral_constant<int, 64>());
