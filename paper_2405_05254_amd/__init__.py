@@ -13,3 +13,4 @@ from .binding import (  # noqa: F401
     PagedCache, rotation_turns, turn_units, paged_append, paged_read, paged_attn, paged_attn_workspace,
     beam_select, beam_select_workspace, beam_reorder_pages, beam_reorder_rows,
 )
+from .beam import BeamSearch  # noqa: F401

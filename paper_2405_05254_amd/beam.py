@@ -1,0 +1,152 @@
+"""Beam search on a YocoStack (Fig. 3 "Generation", W continuations of a prompt at a time) over one global cache in pages.
+
+The beams of a request share the pages of its prompt, and those of the text that they have in common: a beam writes to
+pages of its own, and after every selection takes over its parent's table of pages, with a copy of the one page that is not full
+yet. What the self-decoder keeps of a sequence is small and is moved as it is: rolling windows or retention states of all layers in
+one launch. A step of B requests is one pass of B * W rows: paged_append, paged_attn in every cross-decoder layer, beam_select,
+beam_reorder_pages and beam_reorder_rows; projections, norms and the feed-forward halves are the stack's own.
+"""
+import torch
+
+from . import binding as yb
+
+
+class BeamSearch:
+    """stack: a YocoStack whose kernel dtype is bfloat16; beams: W, up to 16; max_rows: of a sequence, prompt and continuation together;
+    cache_dtype: INT4 or torch.bfloat16, of the pages; eos: the token that ends a beam (-1: none does); rotation_base: the base of
+    a rotation of keys and queries to their positions in the cross-decoder (None: none, as in the stack's own steps)."""
+
+    def __init__(self, stack, beams, max_rows, eos=-1, cache_dtype=yb.INT4, rotation_base=None):
+        if stack.dtype != torch.bfloat16:
+            raise yb.YocoError("the pages are read with bfloat16 queries: a stack of dtype torch.bfloat16, not %s" % stack.dtype)
+        if not 1 <= beams <= 16 or max_rows < 1:
+            raise yb.YocoError("1 to 16 beams and at least one row, not %d and %d" % (beams, max_rows))
+        self.stack, self.W, self.max_rows, self.eos, self.cache_dtype = stack, beams, max_rows, eos, cache_dtype
+        self.turns = None if rotation_base is None else yb.rotation_turns(stack.d, rotation_base, stack.device)
+        self.cache = None
+
+    # -- what a batch of requests keeps
+    def _begin(self, lengths):
+        s, W, dev = self.stack, self.W, self.stack.device
+        rows, cols = len(lengths) * W, -(-self.max_rows // yb.PAGE_ROWS)
+        home, pages = [], 0
+        for n in lengths:                      # beam 0 has the prompt's pages, the others' own begin at the one that it ends in
+            for w in range(W):
+                skip = n // yb.PAGE_ROWS if w else 0
+                home.append([-1] * skip + list(range(pages, pages + cols - skip)))
+                pages += cols - skip
+        self.home = torch.tensor(home, dtype=torch.int32, device=dev)
+        self.table = self.home.view(-1, W, cols)[:, :1].expand(-1, W, cols).reshape(rows, cols).clone()
+        self.cache = yb.PagedCache(pages, s.Hkv, s.d, self.cache_dtype, dev)
+        self.lens = torch.tensor([n for n in lengths for _ in range(W)], dtype=torch.int64, device=dev)
+        self.no_rows = torch.zeros(rows, dtype=torch.int64, device=dev)
+        self.ws_cache = self._workspace(yb.paged_attn_workspace(self.cache, rows, cols, 1, s.Hq))
+        self.ws_ring = None
+        if s.self_kind == "gret":
+            self.rings = [torch.empty(rows, s.Hq, s.d, s.d, dtype=torch.float32, device=dev) for _ in s.self_layers]
+            self.states = self.rings
+        else:
+            self.rings = [yb.KVCache(rows, s.Hkv_self, s.d, s.window, s.dtype, dev) for _ in s.self_layers]
+            self.states = [plane for ring in self.rings for plane in ring.planes()]
+            if self.rings:
+                self.ws_ring = self._workspace(yb.cross_attn_decode_workspace(self.rings[0], s.Hq)[0])
+
+    def _workspace(self, nbytes):
+        return torch.empty(max(16, nbytes), dtype=torch.uint8, device=self.stack.device)
+
+    # -- the pages: K and V of rows that the self-decoder has left, and the cross-decoder's queries
+    def _global_kv(self, X, native):
+        s = self.stack
+        xn = s._norm(X, s.kv["ln"], native)
+        return [(xn @ s.kv[w]).to(s.dtype).view(-1, s.Hkv, s.d) for w in ("W_K", "W_V")]
+
+    def _cross(self, x, table, pos, kv, native, new):
+        """One row a sequence through the cross-decoder, at positions pos. kv: [rows,1,Hkv,d] each; new: they are still to be appended."""
+        s, rows, lens = self.stack, x.shape[0], pos + 1
+        if self.turns is None and new:
+            yb.paged_append(self.cache, table, pos, *kv)
+        for n, L in enumerate(s.cross_layers):
+            def attn(q, n=n):
+                q = q.view(rows, 1, s.Hq, s.d)
+                if self.turns is not None:     # the first layer's queries with the new rows, the others' by themselves
+                    q = yb.paged_append(self.cache, table, pos, *kv, rows=None if new and n == 0 else self.no_rows[:rows], q=q, turns=self.turns)
+                return yb.paged_attn(self.cache, table, q, lens, s.scale, workspace=self.ws_cache)
+            x = s._cross_layer(x, L, attn, native)
+        return s.logits(x)
+
+    def start(self, prompts):
+        """prompts: a 1-d tensor of tokens each. Early-exit prefill of all; returns the logits [B,vocab] of their last positions. All beams of
+        a request stand behind its prompt then, with the states of the first to be taken over (reorder)."""
+        s, W = self.stack, self.W
+        if not len(prompts) or any(p.dim() != 1 or not 0 < p.shape[0] <= self.max_rows for p in prompts):
+            raise yb.YocoError("prompts are 1-d tensors of 1 to %d tokens" % self.max_rows)
+        self._begin([p.shape[0] for p in prompts])
+        native, out = s._current(), []
+        for b, tokens in enumerate(prompts):
+            if s.self_kind == "gret":
+                X = s.self_decoder(tokens, rings=[r[b * W:b * W + 1] for r in self.rings])
+            else:
+                one = [yb.KVCache(1, s.Hkv_self, s.d, s.window, s.dtype, s.device) for _ in s.self_layers]
+                X = s.self_decoder(tokens, rings=one)
+                for ring, of in zip(self.rings, one):
+                    for to, plane in zip(ring.planes(), of.planes()):
+                        to[b * W].copy_(plane[0])
+            T, table = X.shape[0], self.table[b * W:b * W + 1]
+            k, v = self._global_kv(X, native)
+            first = self.no_rows[:1]
+            yb.paged_append(self.cache, table, first, k[None], v[None], turns=self.turns)
+            out.append(self._cross(X[T - 1:].contiguous(), table, first + (T - 1), (k[None, T - 1:], v[None, T - 1:]), native, False))
+        return torch.cat(out)
+
+    def reorder(self, parent):
+        """Every beam becomes what beam parent[b,w] (int32 [B,W]) of its request was."""
+        yb.beam_reorder_pages(self.cache, self.table, self.home, parent, self.lens)
+        if self.states:
+            yb.beam_reorder_rows(self.states, parent)
+
+    def advance(self, token):
+        """token int32 [B,W]: a beam's next one each; returns the logits [B * W,vocab] of what comes after."""
+        s, native, pos = self.stack, self.stack._current(), self.lens
+        lens, x = pos + 1, self.stack.embed[token.reshape(-1)]
+        rows = x.shape[0]
+        for L, ring in zip(s.self_layers, self.rings):
+            xn = s._norm(x, L["ln1"], native)
+            q = (xn @ L["W_Q"]).to(s.dtype).view(rows, s.Hq, s.d)
+            k = (xn @ L["W_K"]).to(s.dtype).view(rows, s.Hkv_self, s.d)
+            v = (xn @ L["W_V"]).to(s.dtype).view(rows, s.Hkv_self, s.d)
+            if s.self_kind == "gret":
+                gate = (xn @ L["W_gate"]).to(s.dtype).view(rows, s.Hq, s.d)
+                o = yb.gret_decode(q, k, v, s._log_decay(xn, L).view(rows, s.Hq), ring, s.scale, group_norm=True, eps=s.eps, gate=gate)
+            else:
+                o = yb.swa_decode(ring, q, lens, s.scale, self.ws_ring, k_new=k, v_new=v)
+            x = s._after_attention(o.view(rows, s.Hq * s.d).to(s.glue), x, L, native)
+        kv = [t[:, None] for t in self._global_kv(x, native)]
+        logits = self._cross(x, self.table, pos, kv, native, True)
+        self.lens = lens
+        return logits
+
+    def generate(self, prompts, steps):
+        """The W best continuations of every prompt by up to `steps` tokens: tokens int32 [B,W,n] (eos behind a beam's end) and scores
+        float32 [B,W], sums of the tokens' log-probabilities, best first. n: steps, or fewer if all beams have ended."""
+        B, W, dev = len(prompts), self.W, self.stack.device
+        if steps < 1 or any(p.shape[0] + steps > self.max_rows + 1 for p in prompts):
+            raise yb.YocoError("a prompt and %d steps do not fit %d rows" % (steps, self.max_rows))
+        logits = self.start(prompts)
+        # behind the prompt there is one beam: the others have no score to come from
+        scores = torch.full((B, W), float("-inf"), device=dev)
+        scores[:, 0] = 0.0
+        logits = logits[:, None].expand(B, W, -1).contiguous()
+        done, ws, chosen = None, self._workspace(yb.beam_select_workspace(B, W, logits.shape[-1])), []
+        for n in range(steps):
+            if n:
+                self.reorder(parent)
+                logits = self.advance(token).view(B, W, -1)
+            parent, token, scores, done = yb.beam_select(logits, scores, done=done, eos=self.eos, workspace=ws)
+            chosen.append((parent, token))
+            if self.eos >= 0 and bool(done.all()):
+                break
+        beam, out = torch.arange(W, device=dev).expand(B, W), []
+        for parent, token in reversed(chosen):           # a beam's tokens from its last one back
+            out.append(token.gather(1, beam))
+            beam = parent.long().gather(1, beam)
+        return torch.stack(out[::-1], dim=2), scores

@@ -1,0 +1,34 @@
+"""What a beam search refuses before it touches the GPU."""
+import pytest
+import torch
+
+import paper_2405_05254_amd as yoco
+import yoco_synth as ys
+from paper_2405_05254_amd.stack import YocoStack
+
+
+def stack(dtype):
+    s = dict(ys.CONFIGS["tiny_fp32"]["stack"], d_model=64, ffn=64, vocab=16)
+    return YocoStack(ys.stack_weights(0, s, "f32"), dtype, device="cpu")
+
+
+def test_beam_search_refuses_what_it_cannot_run():
+    st = stack(torch.bfloat16)
+    with pytest.raises(yoco.YocoError, match="bfloat16"):
+        yoco.BeamSearch(stack(torch.float32), 4, 100)
+    for beams, rows in ((0, 100), (17, 100), (4, 0)):
+        with pytest.raises(yoco.YocoError, match="beams"):
+            yoco.BeamSearch(st, beams, rows)
+    search = yoco.BeamSearch(st, 4, 100)
+    for prompts, steps in (([torch.zeros(90, dtype=torch.int64)], 12), ([torch.zeros(3, dtype=torch.int64)], 0)):
+        with pytest.raises(yoco.YocoError, match="do not fit"):
+            search.generate(prompts, steps)
+    for prompts in ([], [torch.zeros(0, dtype=torch.int64)], [torch.zeros(2, 3, dtype=torch.int64)], [torch.zeros(101, dtype=torch.int64)]):
+        with pytest.raises(yoco.YocoError, match="prompts"):
+            search.start(prompts)
+
+
+@pytest.mark.parametrize("cache_dtype", [torch.float32, torch.int8])
+def test_pages_are_bf16_or_4_bits(cache_dtype):
+    with pytest.raises(yoco.YocoError, match="INT4"):
+        yoco.BeamSearch(stack(torch.bfloat16), 2, 64, cache_dtype=cache_dtype).start([torch.zeros(3, dtype=torch.int64)])
