@@ -667,9 +667,19 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
     auto column_of = [&](int k) { return wave + WAVES * k < columns ? wave + WAVES * k : wave; };
     for (int i0 = 0; i0 < parts; i0 += 64) {
       const float* const at = place(i0 + lane < parts ? i0 + lane : parts - 1);
-      unsigned long long ml[kMine];
+      const int here = parts - i0 < 64 ? parts - i0 : 64;
+      unsigned long long ml[kMine], y[kBatch][kMine];
+      auto fetch = [&](int p) {
+#pragma unroll
+        for (int v = 0; v < kBatch; ++v) {
+          const float* const from = place(i0 + (p + v < here ? p + v : here - 1)) + (e < D ? e : 0);
+#pragma unroll
+          for (int k = 0; k < kMine; ++k) y[v][k] = get_u64(from + column_of(k) * D);
+        }
+      };
 #pragma unroll
       for (int k = 0; k < kMine; ++k) ml[k] = get_u64(at + slot.ml(column_of(k)));
+      fetch(0);
 #pragma unroll
       for (int k = 0; k < kMine; ++k) {
         const float m = i0 + lane < parts ? __uint_as_float((unsigned)ml[k]) : kNegBig;
@@ -680,15 +690,8 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
         o1[k] *= old;
         M[k] = M2;
       }
-      const int here = parts - i0 < 64 ? parts - i0 : 64;
       for (int p = 0; p < here; p += kBatch) {
-        unsigned long long y[kBatch][kMine];
-#pragma unroll
-        for (int v = 0; v < kBatch; ++v) {
-          const float* const from = place(i0 + (p + v < here ? p + v : here - 1)) + (e < D ? e : 0);
-#pragma unroll
-          for (int k = 0; k < kMine; ++k) y[v][k] = get_u64(from + column_of(k) * D);
-        }
+        if (p > 0) fetch(p);
 #pragma unroll
         for (int v = 0; v < kBatch; ++v) {
           if (p + v >= here) break;
