@@ -31,8 +31,14 @@ constexpr float kNegBig = -1.0e30f;      // "no row seen yet": finite, so m - m 
 constexpr int kWholePages = 16;          // as many are not worth a merge, ...
 constexpr int kMinPages = 2;             // ... and a wavefront has no fewer
 constexpr int kManyPages = 8;            // of a wavefront
-constexpr int kWavesPlain = 4;
 constexpr int kAhead4 = 2, kAhead2 = 4, kAheadPlain = 8;
+
+// A value from which nothing is worked out ahead of this place: what the compiler works out for all turns of a loop keeps its registers
+// through all of them.
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
 // What a workgroup takes: pages [p0, p1) of a sequence, for a KV head (and column tile).
 struct Piece {
@@ -164,16 +170,16 @@ struct Args {
   const int64_t* lens;
   float* ws;
   unsigned long long tag;
-  int B, cols, T, Hq, G, tiles, units;   // G: query heads of a KV head; tiles: of 16 columns; units: workgroups that the pages are shared out to
+  int B, cols, T, Hq, G, tiles, units;   // G: query heads of a KV head; tiles: of up to 32 columns; units: workgroups that the pages are shared out to
   float scale;
 };
 
-// What a wavefront knows of its columns (lane n = lane % 16): one softmax state for each lane n.
-template <int D, int NP>
+// What a wavefront knows of its columns: a softmax state for each lane n = lane % 16 and tile of 16 columns.
+template <int D, int NP, int TILES>
 struct State {
-  float m, l;
-  f32x4 o[D / 16];
-  float z[D / 64];                       // 4 bits: sum of p * minimum, this lane's rows
+  float m[TILES], l[TILES];
+  f32x4 o[TILES][D / 16];
+  float z[TILES][D / 64];                // 4 bits: sum of p * minimum, this lane's rows
   int e[NP];                             // 4 bits: exponent field of the largest scale of V that a bank's pages had; its o are relative to 2^(e - 126)
 };
 
@@ -202,18 +208,20 @@ __device__ __forceinline__ u32x4 only(bool mine, u32x4 x) { return (u32x4){mine 
 
 constexpr int kParamStride = 64 * 32 + 32;     // of a page's scales in LDS: the four pages of a read fall in distinct banks
 
-template <int D, int NP, int R>
+template <int D, int NP, int R, int TILES = 1>
 struct Coded {
   static constexpr int kGroups = D / 64, kSteps = D / 32, kLoads = D / 32;        // 16-byte loads of a plane's page
-  static constexpr int kPages = NP, kColumns = 16 / NP;
-  static constexpr int kLds = NP * kParamStride;
+  static constexpr int kPages = NP, kTiles = TILES, kColumns = 16 / NP;       // kColumns: of a tile
+  static constexpr bool kStash = kSteps * TILES > 4;                              // the query lies in LDS: there are no registers for it
+  static constexpr int kLds = NP * kParamStride + (kStash ? kSteps * TILES * 1024 : 0);
   static constexpr int kPlanes = 2 * NP;                                          // of a step: K of its pages, then V
+  static constexpr int kBatch = TILES > 1 ? 4 : 8;                                // rows whose scales are in registers at a time
   static_assert(kPlanes % R == 0, "a plane has its place among R in every step");
   struct Pages {
     u32x4 x[R][kLoads];                  // codes of plane i in x[i % R]; R planes are on their way
     u32x2 k[NP], v[NP];                  // row `lane`'s scales and minima
   };
-  struct Query {
+  struct Query {                         // of a tile
     u32x4 f[kSteps];
     float sum[kGroups], c1, c2;          // of a group's numbers; what turns a sum of products into a score in log2 units
   };
@@ -287,10 +295,19 @@ struct Coded {
     q.c2 = most < 0x7f80u ? exp2i(down - half) : __uint_as_float(0x7fc00000u);                              // a query that is not finite
   }
 
+  static __device__ __forceinline__ void stash(const Query (&q)[TILES], char* lds, int lane) {
+    if constexpr (kStash) {
+#pragma unroll
+      for (int c = 0; c < TILES; ++c)
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) ((u32x4*)(lds + kParamStride))[(c * kSteps + t) * 64 + lane] = q[c].f[t];
+    }
+  }
+
   // NP pages: this lane's column has the page of its bank (lane % 16 / kColumns), of whose rows it sees nv; rows[j]: rows that page j has. now: the pages;
   // next: those of the next step (MORE).
   template <bool MORE>
-  static __device__ __forceinline__ void step(State<D, kPages>& st, const Query& q, Pages& x, int lane, int nv, const int (&rows)[NP], char* lds, const Head& head,
+  static __device__ __forceinline__ void step(State<D, NP, TILES>& st, const Query (&q)[TILES], Pages& x, int lane, const int (&nv)[TILES], const int (&rows)[NP], char* lds, const Head& head,
                                               const int (&now)[NP], const int (&next)[NP]) {
     const int qg = lane >> 4;
     int bank = (lane & 15) / kColumns;
@@ -312,105 +329,140 @@ struct Coded {
       if (MORE) load_params(x, j, head.k_of(next[j]), head.v_of(next[j]), lane);
     }
     __builtin_amdgcn_sched_barrier(0);
-    f32x4 acc[4][kGroups];
-#pragma unroll
-    for (int tau = 0; tau < 4; ++tau)
-#pragma unroll
-      for (int h = 0; h < kGroups; ++h) acc[tau][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      u32x4 f[kSteps];
-#pragma unroll
-      for (int t = 0; t < kSteps; ++t) f[t] = NP > 1 ? only(bank == j, q.f[t]) : q.f[t];
-#pragma unroll
-      for (int tau = 0; tau < 4; ++tau) {
-#pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
-          const int i = tau * kSteps + t;
-          acc[tau][t / 2] = mfma_f16(nibbles_k(x.x[j % R][i / 4][i % 4]), f[t], acc[tau][t / 2]);
-        }
-        __builtin_amdgcn_sched_barrier(0);                               // few operands at a time, and the loads go where the codes were
-      }
-      refill<MORE>(x, j, head, now, next, lane);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    // scores of rows 16 tau + 4 qg + i of the bank's page
-    float s[16], smax = -INFINITY;
+    // scores of rows 16 tau + 4 qg + i of the bank's page; of two tiles 32 rows at a time, for the registers
+    constexpr int kSlices = TILES > 1 ? 2 : 1, kTau = 4 / kSlices;
+    float s[TILES][16], m_new[TILES];
     const char* const mine = lds + bank * kParamStride + qg * 128;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      f32x4 par[8];
+    for (int slice = 0; slice < kSlices; ++slice) {
+      f32x4 acc[TILES][kTau][kGroups];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) par[r] = *(const f32x4*)(mine + ((half * 2 + r / 4) * 16 + r % 4) * 32);
-      __builtin_amdgcn_sched_barrier(0);                                 // one wait for all
+      for (int c = 0; c < TILES; ++c)
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        float a = par[r][1] * q.sum[0];
-        a = fmaf(par[r][0], acc[half * 2 + r / 4][0][r % 4], a);
-        if constexpr (kGroups > 1) {
-          a = fmaf(par[r][3], q.sum[1], a);
-          a = fmaf(par[r][2], acc[half * 2 + r / 4][1][r % 4], a);
+        for (int tau = 0; tau < kTau; ++tau)
+#pragma unroll
+          for (int h = 0; h < kGroups; ++h) acc[c][tau][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        u32x4 f[TILES][kSteps];
+#pragma unroll
+        for (int c = 0; c < TILES; ++c)
+#pragma unroll
+          for (int t = 0; t < kSteps; ++t) {
+            if constexpr (kStash) f[c][t] = ((const u32x4*)(lds + kParamStride))[(c * kSteps + t) * 64 + lane];
+            else f[c][t] = NP > 1 ? only(bank == j, q[c].f[t]) : q[c].f[t];
+          }
+#pragma unroll
+        for (int tau = 0; tau < kTau; ++tau) {
+#pragma unroll
+          for (int t = 0; t < kSteps; ++t) {
+            const int i = (slice * kTau + tau) * kSteps + t;
+            const u32x4 codes = nibbles_k(x.x[j % R][i / 4][i % 4]);
+#pragma unroll
+            for (int c = 0; c < TILES; ++c) acc[c][tau][t / 2] = mfma_f16(codes, f[c][t], acc[c][tau][t / 2]);
+          }
+          __builtin_amdgcn_sched_barrier(0);                             // few operands at a time, and the loads go where the codes were
         }
-        s[half * 8 + r] = a * q.c1 * q.c2;
+        if (slice == kSlices - 1) refill<MORE>(x, j, head, now, next, lane);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int at = 0; at < kTau * 4; at += kBatch) {
+        f32x4 par[kBatch];
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) par[r] = *(const f32x4*)(mine + ((slice * kTau + (at + r) / 4) * 16 + r % 4) * 32);
+        __builtin_amdgcn_sched_barrier(0);                               // one wait for all
+#pragma unroll
+        for (int c = 0; c < TILES; ++c)
+#pragma unroll
+          for (int r = 0; r < kBatch; ++r) {
+            float a = par[r][1] * q[c].sum[0];
+            a = fmaf(par[r][0], acc[c][(at + r) / 4][0][r % 4], a);
+            if constexpr (kGroups > 1) {
+              a = fmaf(par[r][3], q[c].sum[1], a);
+              a = fmaf(par[r][2], acc[c][(at + r) / 4][1][r % 4], a);
+            }
+            s[c][slice * kTau * 4 + at + r] = a * q[c].c1 * q[c].c2;
+          }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (__builtin_amdgcn_ballot_w64(nv < kPageRows)) {                   // the end of a sequence, or no page
+    u32x4 b[TILES][kGroups][2];
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (r / 4 * 16 + qg * 4 + r % 4 >= nv) s[r] = -INFINITY;
+    for (int c = 0; c < TILES; ++c) {
+      if (__builtin_amdgcn_ballot_w64(nv[c] < kPageRows)) {              // the end of a sequence, or no page
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (r / 4 * 16 + r % 4 >= nv[c] - qg * 4) s[c][r] = -INFINITY;
+      }
+      float smax = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) smax = fmaxf(smax, s[c][r]);
+      m_new[c] = fmaxf(st.m[c], over_rows<LaneMax>(smax));               // the four lanes of a column hold 16 rows each
+      if (larger || __builtin_amdgcn_ballot_w64(m_new[c] != st.m[c])) {  // rare once the stream has met its large scores
+        int e = e_old[0] - st.e[0];
+#pragma unroll
+        for (int j = 1; j < NP; ++j)
+          if (const int other = __builtin_amdgcn_readfirstlane(e_old[j] - st.e[j]); bank == j) e = other;
+        const float alpha = __builtin_amdgcn_exp2f(st.m[c] - m_new[c]), beta = __builtin_amdgcn_exp2f(st.m[c] - m_new[c] + (float)e);
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) st.o[c][t] *= beta;
+#pragma unroll
+        for (int h = 0; h < kGroups; ++h) st.z[c][h] *= alpha;
+        st.l[c] *= alpha;
+        st.m[c] = m_new[c];
+      }
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) smax = fmaxf(smax, s[r]);
-    const float m_new = fmaxf(st.m, over_rows<LaneMax>(smax));           // the four lanes of a column hold 16 rows each
-    if (larger || __builtin_amdgcn_ballot_w64(m_new != st.m)) {   // rare once the stream has met its large scores
-      int e = e_old[0] - st.e[0];
+    for (int at = 0; at < 16; at += kBatch) {
+      f32x4 par[kBatch];
 #pragma unroll
-      for (int j = 1; j < NP; ++j)
-        if (const int other = __builtin_amdgcn_readfirstlane(e_old[j] - st.e[j]); bank == j) e = other;
-      const float alpha = __builtin_amdgcn_exp2f(st.m - m_new), beta = __builtin_amdgcn_exp2f(st.m - m_new + (float)e);
-#pragma unroll
-      for (int t = 0; t < D / 16; ++t) st.o[t] *= beta;
-#pragma unroll
-      for (int h = 0; h < kGroups; ++h) st.z[h] *= alpha;
-      st.l *= alpha;
-      st.m = m_new;
-    }
-    u32x4 b[kGroups][2];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      float w[kGroups][8];
-      f32x4 par[8];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) par[r] = *(const f32x4*)(mine + ((half * 2 + r / 4) * 16 + r % 4) * 32 + 16);
+      for (int r = 0; r < kBatch; ++r) par[r] = *(const f32x4*)(mine + ((at + r) / 4 * 16 + r % 4) * 32 + 16);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const float p = __builtin_amdgcn_exp2f(s[half * 8 + r] - m_new);
-        st.l += p;
+      for (int c = 0; c < TILES; ++c)
 #pragma unroll
-        for (int h = 0; h < kGroups; ++h) {
-          w[h][r] = p * par[r][2 * h];
-          st.z[h] = fmaf(p, par[r][2 * h + 1], st.z[h]);
+        for (int r0 = 0; r0 < kBatch; r0 += 4) {
+          float w[kGroups][4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float p = __builtin_amdgcn_exp2f(s[c][at + r0 + r] - m_new[c]);
+            st.l[c] += p;
+#pragma unroll
+            for (int h = 0; h < kGroups; ++h) {
+              w[h][r] = p * par[r0 + r][2 * h];
+              st.z[c][h] = fmaf(p, par[r0 + r][2 * h + 1], st.z[c][h]);
+            }
+          }
+#pragma unroll
+          for (int h = 0; h < kGroups; ++h) {
+            b[c][h][(at + r0) / 8][(at + r0) / 4 % 2 * 2] = pack_f16(w[h][0], w[h][2]);
+            b[c][h][(at + r0) / 8][(at + r0) / 4 % 2 * 2 + 1] = pack_f16(w[h][1], w[h][3]);
+          }
         }
-      }
-#pragma unroll
-      for (int h = 0; h < kGroups; ++h)
-        b[h][half] = (u32x4){pack_f16(w[h][0], w[h][2]), pack_f16(w[h][1], w[h][3]), pack_f16(w[h][4], w[h][6]), pack_f16(w[h][5], w[h][7])};
+      if (TILES > 1) __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-      u32x4 f[kGroups][2];
+      u32x4 f[TILES][kGroups][2];
 #pragma unroll
-      for (int h = 0; h < kGroups; ++h)
+      for (int c = 0; c < TILES; ++c)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) f[h][half] = NP > 1 ? only(bank == j, b[h][half]) : b[h][half];
+        for (int h = 0; h < kGroups; ++h)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) f[c][h][half] = NP > 1 ? only(bank == j, b[c][h][half]) : b[c][h][half];
 #pragma unroll
       for (int t = 0; t < kLoads; ++t) {                                 // 32 dimensions: the low nibbles are 16 of them, the high ones the others
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const unsigned w0 = x.x[(NP + j) % R][t][half * 2], w1 = x.x[(NP + j) % R][t][half * 2 + 1], u0 = w0 >> 8, u1 = w1 >> 8;
-          st.o[2 * t] = mfma_f16((u32x4){w0 & 0x000f000fu, u0 & 0x000f000fu, w1 & 0x000f000fu, u1 & 0x000f000fu}, f[t / 2][half], st.o[2 * t]);
-          st.o[2 * t + 1] = mfma_f16((u32x4){w0 & 0x00f000f0u, u0 & 0x00f000f0u, w1 & 0x00f000f0u, u1 & 0x00f000f0u}, f[t / 2][half], st.o[2 * t + 1]);
+          const u32x4 low = {w0 & 0x000f000fu, u0 & 0x000f000fu, w1 & 0x000f000fu, u1 & 0x000f000fu};
+          const u32x4 high = {w0 & 0x00f000f0u, u0 & 0x00f000f0u, w1 & 0x00f000f0u, u1 & 0x00f000f0u};
+#pragma unroll
+          for (int c = 0; c < TILES; ++c) {
+            st.o[c][2 * t] = mfma_f16(low, f[c][t / 2][half], st.o[c][2 * t]);
+            st.o[c][2 * t + 1] = mfma_f16(high, f[c][t / 2][half], st.o[c][2 * t + 1]);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -420,27 +472,29 @@ struct Coded {
   }
 
   // The state's vector as it is: dimensions 16 t + 4 qg + i.
-  static __device__ __forceinline__ void finish(State<D, kPages>& st, int bank) {
+  static __device__ __forceinline__ void finish(State<D, NP, TILES>& st, int bank) {
     int e = st.e[0];
 #pragma unroll
     for (int j = 1; j < NP; ++j)
       if (const int other = __builtin_amdgcn_readfirstlane(st.e[j]); bank == j) e = other;
     const float up = exp2i(e - 126 + 24);
 #pragma unroll
-    for (int h = 0; h < kGroups; ++h) {
-      const float z = over_rows<LaneSum>(st.z[h]);
+    for (int c = 0; c < TILES; ++c)
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int h = 0; h < kGroups; ++h) {
+        const float z = over_rows<LaneSum>(st.z[c][h]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) st.o[h * 4 + t][i] = fmaf(st.o[h * 4 + t][i], t % 2 ? up * 0.0625f : up, z);
-    }
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st.o[c][h * 4 + t][i] = fmaf(st.o[c][h * 4 + t][i], t % 2 ? up * 0.0625f : up, z);
+      }
   }
 };
 
 // ---- bf16 pages: softmax weights go in as a bf16 high part and a bf16 remainder (two products), which keeps 16 bits of them
-template <int D, int R>
+template <int D, int R, int TILES = 1>
 struct Plain {
-  static constexpr int kSteps = D / 32, kLoads = D / 8, kPages = 1, kColumns = 16, kLds = 16;
+  static constexpr int kSteps = D / 32, kLoads = D / 8, kPages = 1, kTiles = TILES, kColumns = 16, kLds = 16;
   static_assert(kLoads % R == 0, "a piece has its place among R in either plane");
   struct Pages {
     u32x4 x[R];                          // 1 KiB pieces of K, then of V: piece i in x[i % R], R of them on their way
@@ -460,52 +514,62 @@ struct Plain {
     for (int t = 0; t < kSteps; ++t) q.f[t] = raw[t];
     q.scale = scale * kLog2e;
   }
-    template <bool MORE>
-  static __device__ __forceinline__ void step(State<D, kPages>& st, const Query& q, Pages& x, int lane, int nv, const int (&rows)[1], char*, const Head& head, const int (&now)[1],
-                                              const int (&next)[1]) {
+  template <bool MORE>
+  static __device__ __forceinline__ void step(State<D, 1, TILES>& st, const Query (&q)[TILES], Pages& x, int lane, const int (&nv)[TILES], const int (&rows)[1], char*, const Head& head,
+                                              const int (&now)[1], const int (&next)[1]) {
     const char *const k = head.k_of(now[0]), *const v = head.v_of(now[0]), *const k2 = head.k_of(next[0]);
     const int qg = lane >> 4;
-    float s[16];
-    float smax = -INFINITY;
+    float s[TILES][16];
 #pragma unroll
     for (int tau = 0; tau < 4; ++tau) {
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      f32x4 acc[TILES];
+#pragma unroll
+      for (int c = 0; c < TILES; ++c) acc[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int t = 0; t < kSteps; ++t) {
         const int i = tau * kSteps + t;
-        acc = mfma_bf16(x.x[i % R], q.f[t], acc);
+#pragma unroll
+        for (int c = 0; c < TILES; ++c) acc[c] = mfma_bf16(x.x[i % R], q[c].f[t], acc[c]);
         x.x[i % R] = i + R < kLoads ? piece(k, i + R, lane) : piece(v, i + R - kLoads, lane);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float a = acc[i] * q.scale;
-        if (tau * 16 + qg * 4 + i >= nv) a = -INFINITY;
-        s[tau * 4 + i] = a;
-        smax = fmaxf(smax, a);
-      }
-    }
-    const float m_new = fmaxf(st.m, over_rows<LaneMax>(smax));
-    if (__builtin_amdgcn_ballot_w64(m_new != st.m)) {
-      const float alpha = __builtin_amdgcn_exp2f(st.m - m_new);
+      for (int c = 0; c < TILES; ++c)
 #pragma unroll
-      for (int t = 0; t < D / 16; ++t) st.o[t] *= alpha;
-      st.l *= alpha;
-      st.m = m_new;
+        for (int i = 0; i < 4; ++i) s[c][tau * 4 + i] = tau * 16 + i >= nv[c] - qg * 4 ? -INFINITY : acc[c][i] * q[c].scale;
     }
-    u32x4 hi[2], lo[2], there[2];
+    u32x4 hi[TILES][2], lo[TILES][2], there[2];
+#pragma unroll
+    for (int c = 0; c < TILES; ++c) {
+      float smax = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) smax = fmaxf(smax, s[c][r]);
+      const float m_new = fmaxf(st.m[c], over_rows<LaneMax>(smax));
+      if (__builtin_amdgcn_ballot_w64(m_new != st.m[c])) {
+        const float alpha = __builtin_amdgcn_exp2f(st.m[c] - m_new);
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) st.o[c][t] *= alpha;
+        st.l[c] *= alpha;
+        st.m[c] = m_new;
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const float a = __builtin_amdgcn_exp2f(s[c][half * 8 + 2 * p] - m_new), b = __builtin_amdgcn_exp2f(s[c][half * 8 + 2 * p + 1] - m_new);
+          st.l[c] += a;
+          st.l[c] += b;
+          const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
+          const float ra = a - __uint_as_float(ua & 0xffff0000u), rb = b - __uint_as_float(ub & 0xffff0000u);
+          hi[c][half][p] = (ua >> 16) | (ub & 0xffff0000u);
+          lo[c][half][p] = (__float_as_uint(ra) >> 16) | (__float_as_uint(rb) & 0xffff0000u);
+        }
+    }
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
-        const float a = __builtin_amdgcn_exp2f(s[half * 8 + 2 * p] - m_new), b = __builtin_amdgcn_exp2f(s[half * 8 + 2 * p + 1] - m_new);
-        st.l += a;
-        st.l += b;
-        const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
-        const float ra = a - __uint_as_float(ua & 0xffff0000u), rb = b - __uint_as_float(ub & 0xffff0000u);
-        hi[half][p] = (ua >> 16) | (ub & 0xffff0000u);
-        lo[half][p] = (__float_as_uint(ra) >> 16) | (__float_as_uint(rb) & 0xffff0000u);
-        const int r = (half * 2 + p / 2) * 16 + qg * 4 + p % 2 * 2;      // rows that the page does not have hold whatever the memory held
-        there[half][p] = (r < rows[0] ? 0x0000ffffu : 0u) | (r + 1 < rows[0] ? 0xffff0000u : 0u);
+        const int r = (half * 2 + p / 2) * 16 + p % 2 * 2, end = rows[0] - qg * 4;      // rows that the page does not have hold whatever the memory held
+        there[half][p] = (r < end ? 0x0000ffffu : 0u) | (r + 1 < end ? 0xffff0000u : 0u);
       }
 #pragma unroll
     for (int t = 0; t < D / 16; ++t)
@@ -513,64 +577,76 @@ struct Plain {
       for (int half = 0; half < 2; ++half) {
         const int i = t * 2 + half;
         const u32x4 w = x.x[i % R] & there[half];
-        st.o[t] = mfma_bf16(w, hi[half], st.o[t]);
-        st.o[t] = mfma_bf16(w, lo[half], st.o[t]);
+#pragma unroll
+        for (int c = 0; c < TILES; ++c) {
+          st.o[c][t] = mfma_bf16(w, hi[c][half], st.o[c][t]);
+          st.o[c][t] = mfma_bf16(w, lo[c][half], st.o[c][t]);
+        }
         if (i + R < kLoads) x.x[i % R] = piece(v, i + R, lane);
         else if (MORE) x.x[i % R] = piece(k2, i + R - kLoads, lane);
       }
   }
-  static __device__ __forceinline__ void finish(State<D, 1>&, int) {}
+  static __device__ __forceinline__ void stash(const Query (&)[TILES], char*, int) {}
+  static __device__ __forceinline__ void finish(State<D, 1, TILES>&, int) {}
 };
 
 __device__ __forceinline__ unsigned pair_bf16(float a, float b) { return (unsigned)f32_to_bf16(a) | ((unsigned)f32_to_bf16(b) << 16); }
 
-template <int D, int WAVES>
+template <int D, int WAVES, int TILES>
 struct Merge {
-  float o[WAVES][16][D + 4], ml[WAVES][16][2];
+  float o[WAVES][16 * TILES][D + 4], ml[WAVES][16 * TILES][2];
 };
 // The states that are merged at the end lie where the scales of the pages were.
 template <int D, int WAVES, typename Form>
 union Lds {
   char params[WAVES * Form::kLds];
-  Merge<D, WAVES> red;
+  Merge<D, WAVES, Form::kTiles> red;
 };
 
 template <int D, int WAVES, typename Form>
-__device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict__ table, const Piece& piece, Merge<D, WAVES>& red, char* params) {
-  constexpr int NP = Form::kPages, NC = Form::kColumns;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+__device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict__ table, const Piece& piece, Merge<D, WAVES, Form::kTiles>& red, char* params) {
+  constexpr int NP = Form::kPages, NC = Form::kColumns, TILES = Form::kTiles, kMost = NC * TILES;
+  const int thread = here(threadIdx.x), wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = thread & 63;
   const int n = lane & 15, qg = lane >> 4, bank = n / NC;
   const size_t page_size = page_bytes(D, a.c.dtype);
-  const Slot<D> slot = {a.tiles > 1 ? 16 : a.T * a.G};
+  const Slot<D> slot = {a.tiles > 1 ? kMost : a.T * a.G};
   const int b = piece.b, len = piece.len, p1 = piece.p1;
   const int g = a.tiles > 1 ? __builtin_amdgcn_readfirstlane(piece.head / a.tiles) : piece.head, tile = piece.head - g * a.tiles;
 
-  // this lane's column: row ti and head of the query, and how many rows it sees
-  const int column = tile * 16 + n % NC, columns = a.T * a.G - tile * 16 < NC ? a.T * a.G - tile * 16 : NC;
-  const bool there = n % NC < columns;
-  const int ti = a.T > 1 ? column / a.G : 0, seen = there ? len - a.T + 1 + ti : len;
-  u32x4 raw[Form::kSteps] = {};
-  if (there) {
-    const bf16_t* const qp = a.q + (((int64_t)b * a.T + ti) * a.Hq + g * a.G + (column - ti * a.G)) * D + qg * 8;
+  // this lane's columns, one of each tile: row ti and head of the query, and how many rows it sees
+  const int columns = a.T * a.G - tile * kMost < kMost ? a.T * a.G - tile * kMost : kMost;
+  u32x4 raw[TILES][Form::kSteps] = {};
+  int seen[TILES];
 #pragma unroll
-    for (int t = 0; t < Form::kSteps; ++t) raw[t] = *(const u32x4*)(qp + t * 32);
+  for (int c = 0; c < TILES; ++c) {
+    const int column = tile * kMost + c * 16 + n % NC, ti = a.T > 1 ? column / a.G : 0;
+    const bool there = c * 16 + n % NC < columns;
+    seen[c] = there ? len - a.T + 1 + ti : len;
+    if (there) {
+      const bf16_t* const qp = a.q + (((int64_t)b * a.T + ti) * a.Hq + g * a.G + (column - ti * a.G)) * D + qg * 8;
+#pragma unroll
+      for (int t = 0; t < Form::kSteps; ++t) raw[c][t] = *(const u32x4*)(qp + t * 32);
+    }
   }
 
   const int32_t* const row = table + (int64_t)b * a.cols;
   const Head head = {(const char*)a.c.k + (size_t)g * page_size, (const char*)a.c.v + (size_t)g * page_size, page_size * a.c.Hkv};
   typename Form::Pages x;
-  State<D, NP> st;
-  st.m = kNegBig;
-  st.l = 0.f;
+  State<D, NP, TILES> st;
+  typename Form::Query q[TILES];
 #pragma unroll
   for (int j = 0; j < NP; ++j) st.e[j] = 0;
 #pragma unroll
-  for (int t = 0; t < D / 16; ++t) st.o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < TILES; ++c) {
+    st.m[c] = kNegBig;
+    st.l[c] = 0.f;
 #pragma unroll
-  for (int h = 0; h < D / 64; ++h) st.z[h] = 0.f;
-
-  typename Form::Query q;
-  Form::prepare(q, raw, a.scale);
+    for (int t = 0; t < D / 16; ++t) st.o[c][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) st.z[c][h] = 0.f;
+    Form::prepare(q[c], raw[c], a.scale);
+  }
+  Form::stash(q, params + wave * Form::kLds, lane);
   // A wavefront's pages, 64 at a time: a lane has the entry of the table for one of them. In the loop nothing is loaded under a
   // condition, so that every wait is for the oldest loads alone.
   for (int p0 = piece.p0 + wave; p0 < p1; p0 += 64 * WAVES) {
@@ -578,7 +654,7 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
     const bool is = mine < p1 && id >= 0 && id < a.c.n_pages;
     const int page = is ? id : 0, has = is ? left < kPageRows ? left : kPageRows : -1;       // -1: no such page
     const int count = (p1 - p0 + WAVES - 1) / WAVES < 64 ? (p1 - p0 + WAVES - 1) / WAVES : 64;
-    int now[NP], next[NP], rows[NP], nv;
+    int now[NP], next[NP], rows[NP], nv[TILES];
 #pragma unroll
     for (int j = 0; j < NP; ++j) now[j] = __builtin_amdgcn_readlane(page, j);
     Form::begin(x, head, now, lane);
@@ -586,7 +662,9 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
         rows[j] = __builtin_amdgcn_readlane(has, i + j);
-        if (NP == 1 || bank == j) nv = rows[j] < 0 ? 0 : seen - (p0 + WAVES * (i + j)) * kPageRows;
+#pragma unroll
+        for (int c = 0; c < TILES; ++c)
+          if (NP == 1 || bank == j) nv[c] = rows[j] < 0 ? 0 : seen[c] - (p0 + WAVES * (i + j)) * kPageRows;
       }
     };
     int i = 0;
@@ -602,13 +680,18 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
     Form::template step<false>(st, q, x, lane, nv, rows, params + wave * Form::kLds, head, now, now);
   }
   Form::finish(st, bank);
-  const float l = over_rows<LaneSum>(st.l);
+  float l[TILES];
+#pragma unroll
+  for (int c = 0; c < TILES; ++c) l[c] = over_rows<LaneSum>(st.l[c]);
   __syncthreads();
 #pragma unroll
-  for (int t = 0; t < D / 16; ++t) *(f32x4*)&red.o[wave][n][t * 16 + qg * 4] = st.o[t];
-  if (qg == 0) {
-    red.ml[wave][n][0] = st.m;
-    red.ml[wave][n][1] = l;
+  for (int c = 0; c < TILES; ++c) {
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) *(f32x4*)&red.o[wave][c * 16 + n][t * 16 + qg * 4] = st.o[c][t];
+    if (qg == 0) {
+      red.ml[wave][c * 16 + n][0] = st.m[c];
+      red.ml[wave][c * 16 + n][1] = l[c];
+    }
   }
   __syncthreads();
 
@@ -619,7 +702,7 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
   float* const mine = place(piece.part);
   auto store = [&](int c, float o0, float o1, float sum) {               // no row seen: zeros
     if (e >= D) return;
-    const int col = tile * 16 + c, t = a.T > 1 ? col / a.G : 0;
+    const int col = tile * kMost + c, t = a.T > 1 ? col / a.G : 0;
     const float inv = opaque_bits(sum) ? 1.f / sum : 0.f;
     *(unsigned*)(a.o + (((int64_t)b * a.T + t) * a.Hq + g * a.G + (col - t * a.G)) * D + e) = pair_bf16(o0 * inv, o1 * inv);
   };
@@ -657,7 +740,7 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
   if (__builtin_amdgcn_ballot_w64(!all_there)) return;
   // All of the wavefront's columns at once, 64 parts at a time: a lane has the maxima and sums of one of them.
   auto merge = [&](auto most) {
-    constexpr int kMine = decltype(most)::value, kBatch = kMine > 2 ? 8 : 16;
+    constexpr int kMine = decltype(most)::value, kBatch = kMine > 2 ? 32 / kMine : 16;
     float M[kMine], sum[kMine], o0[kMine], o1[kMine], f[kMine];
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
@@ -710,7 +793,8 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
   };
   if (columns <= WAVES) merge(std::integral_constant<int, 1>());
   else if (columns <= 2 * WAVES) merge(std::integral_constant<int, 2>());
-  else merge(std::integral_constant<int, 16 / WAVES>());
+  else if (columns <= 4 * WAVES) merge(std::integral_constant<int, 4>());
+  else merge(std::integral_constant<int, 8>());
   for (int i = lane; i < parts; i += 64) put_u64(place(i) + slot.tag(wave), 0ull);       // a captured launch can be replayed
 }
 
@@ -744,49 +828,61 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(Args a, const int32
   }
 }
 
-// Wavefronts of a workgroup and workgroups that the pages are shared out to, of 4 bits two wavefronts a SIMD in all. With 8 there are half as many
-// parts to merge; with 4 workgroups overlap, and shorter pieces are had. 8 where every piece is part of something longer:
-// 3 x 20000 rows, 24 pairs of sequence and KV head: 17.6 us, with 4 20.5; 64 x 1000, 512 pairs: 19.8, with 4 14.1; 8 x 3000, 64 pairs of few pages: 14.9, with 4 12.2.
+// How a call is run: columns of a workgroup (two tiles of 16, or one: of up to 16), wavefronts of one, and workgroups that the pages are shared out
+// to, of 4 bits two wavefronts a SIMD in all.
+// Two tiles take the codes apart (or read the pages) once for both, but half as many pairs of sequence and heads are cut into twice as many parts, so
+// that there has to be enough of them for every compute unit. 4 bits, 8 KV heads of 4: 3 sequences x 20000, 64 rows, 234 pages a compute unit: 118
+// us, with one tile 136; 16 x 2000, 6 rows, 16 pages: 27, with one 20.4. bf16: 16 x 2000, 6 rows: 24.9, with one 35.6; 4 x 2000, 4 pages: 19.0, with one 16.9.
+// With 8 wavefronts there are half as many parts to merge; with 4 workgroups overlap, and shorter pieces are had. 8 where every piece is part of
+// something longer: 3 x 20000, 24 pairs: 17.5 us, with 4 20.5; 64 x 1000, 512 pairs: 19.8, with 4 14.1; 8 x 3000, 64 pairs of few pages: 14.9, with 4
+// 12.5.
 struct Plan {
-  int waves, units;
+  int columns, tiles, waves, units;
+  int64_t segments;
 };
-Plan attn_plan(int dtype, int64_t segments, int cols) {
-  const int cus = compute_units();
-  if (dtype != YOCO_INT4) return {kWavesPlain, cus};
-  const bool eight = segments * 2 < cus && segments * cols >= 16 * (int64_t)cus;
-  return {eight ? 8 : 4, eight ? cus : 2 * cus};
+Plan attn_plan(const PagedAttnView& a) {
+  const int cus = compute_units(), all = a.T * (a.Hq / a.c.Hkv);
+  const int64_t pairs = (int64_t)a.B * a.c.Hkv;
+  Plan p;
+  const int64_t work = pairs * ((all + 31) / 32) * a.cols / cus;           // pages
+  const int wide = work >= (a.c.dtype == YOCO_INT4 ? 128 : 16) ? 32 : 16;
+  p.columns = all < wide ? all : wide;
+  p.tiles = (all + wide - 1) / wide;
+  p.segments = pairs * p.tiles;
+  p.waves = a.c.dtype == YOCO_INT4 && p.segments * 2 < cus && p.segments * a.cols >= 16 * (int64_t)cus ? 8 : 4;
+  p.units = a.c.dtype == YOCO_INT4 && p.waves == 4 ? 2 * cus : cus;
+  return p;
 }
-int64_t segments_of(const PagedAttnView& a) { return (int64_t)a.B * a.c.Hkv * ((a.T * (a.Hq / a.c.Hkv) + 15) / 16); }
 
 }  // namespace
 
-// Rounding a sequence's last piece up makes at most one more for each sequence and head; of those that are cut there are at most twice as many pieces
+// Rounding a sequence's lane piece up makes at most one more for each sequence and head; of those that are cut there are at most twice as many pieces
 // as shares.
 size_t paged_attn_workspace(const PagedAttnView& a) {
-  const int G = a.Hq / a.c.Hkv, columns = a.T * G < 16 ? a.T * G : 16;
-  const size_t floats = a.c.d == 128 ? Slot<128>{columns}.floats() : Slot<64>{columns}.floats();
-  return (size_t)2 * attn_plan(a.c.dtype, segments_of(a), a.cols).units * floats * sizeof(float);
+  const Plan p = attn_plan(a);
+  const size_t floats = a.c.d == 128 ? Slot<128>{p.columns}.floats() : Slot<64>{p.columns}.floats();
+  return (size_t)2 * p.units * floats * sizeof(float);
 }
 
 hipError_t launch_paged_attn(const PagedAttnView& v, void* workspace, unsigned long long tag, hipStream_t s) {
-  const int G = v.Hq / v.c.Hkv, columns = v.T * G, tiles = (columns + 15) / 16;
-  const int64_t segments = segments_of(v);
-  const Plan plan = attn_plan(v.c.dtype, segments, v.cols);
-  const Args a = {v.c, (const bf16_t*)v.q, (bf16_t*)v.o, v.lens, (float*)workspace, tag, v.B, v.cols, v.T, v.Hq, G, tiles, plan.units, v.scale};
+  const Plan p = attn_plan(v);
+  const Args a = {v.c, (const bf16_t*)v.q, (bf16_t*)v.o, v.lens, (float*)workspace, tag, v.B, v.cols, v.T, v.Hq, v.Hq / v.c.Hkv, p.tiles, p.units, v.scale};
   // no more pieces than pages
-  const int64_t most = segments * ((v.cols + plan.waves * kMinPages - 1) / (plan.waves * kMinPages));
-  const dim3 grid((unsigned)(segments + plan.units < most ? segments + plan.units : most));
-  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * plan.waves), 0, s, a, v.table); };
+  const int64_t most = p.segments * ((v.cols + p.waves * kMinPages - 1) / (p.waves * kMinPages));
+  const dim3 grid((unsigned)(p.segments + p.units < most ? p.segments + p.units : most));
+  auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * p.waves), 0, s, a, v.table); };
   auto coded = [&](auto d, auto waves) {
     constexpr int D = decltype(d)::value, WAVES = decltype(waves)::value;
-    if (columns <= 4) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 4, kAhead4>>);
-    else if (columns <= 8) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 2, kAhead2>>);
-    else go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 1, 2>>);
+    if (p.columns <= 4) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 4, kAhead4>>);
+    else if (p.columns <= 8) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 2, kAhead2>>);
+    else if (p.columns <= 16) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 1, 2>>);
+    else go(&attn_kernel<D, WAVES, Coded<D, 1, 2, 2>, Coded<D, 1, 2, 2>>);
   };
   auto by_d = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (v.c.dtype != YOCO_INT4) go(&attn_kernel<D, kWavesPlain, Plain<D, kAheadPlain>, Plain<D, kAheadPlain>>);
-    else if (plan.waves == 8) coded(d, std::integral_constant<int, 8>());
+    if (v.c.dtype != YOCO_INT4 && p.columns <= 16) go(&attn_kernel<D, 4, Plain<D, kAheadPlain>, Plain<D, kAheadPlain>>);
+    else if (v.c.dtype != YOCO_INT4) go(&attn_kernel<D, 4, Plain<D, kAheadPlain, 2>, Plain<D, kAheadPlain, 2>>);
+    else if (p.waves == 8) coded(d, std::integral_constant<int, 8>());
     else coded(d, std::integral_constant<int, 4>());
   };
   if (v.c.d == 128) by_d(std::integral_constant<int, 128>());
