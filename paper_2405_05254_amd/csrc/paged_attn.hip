@@ -1,12 +1,16 @@
 // Attention over a cache in pages: o = softmax(scale q.k) v for the last T rows of every sequence, causal, d 64 or 128, bf16 or
-// 4-bit pages. HBM-bound: every page is read once for all query heads of its KV head and up to 16 / G rows of the query.
+// 4-bit pages. With few rows it is bound by memory: every page is read once for all query heads of its KV head and the rows of the query that a
+// workgroup has. A step of one token, 24 query heads on 8 KV heads of 128 dimensions: 16 sequences x 32768, 4 bits: 98 us for 604 MB (6.2 TB/s; the
+// loads by themselves, in this order, take 93), bf16 318 us (6.7 TB/s); 1 x 524288, 4 bits: 98 us. Of short sequences the time is that of a
+// dependent chain, and of the merge: 8 x 3000: 12.5 us, 1 x 200: 6.4. With many rows the vector instructions bound it that take the codes apart and
+// form the weights: 64 rows of 32 heads over 3 x 20000: 104 us, 404 TFLOP/s.
 //
-// Work. The pages of all sequences and KV heads (and, of more than 16 columns = rows x heads of a KV head, column tiles) in a row
-// are cut into as many equal ranges as there are workgroups, so that ragged lengths end together. A range may hold the
-// end of one (sequence, head), whole ones, and the beginning of another; what is not whole goes to the workspace and is
-// merged by whoever finds all of it published (decode_tail.h says how that works without waiting or clearing).
+// Work. The pages of all sequences and KV heads (and, of more columns = rows x heads of a KV head than a workgroup has, tiles of columns) are
+// shared out in one of two ways. Many pages, in a row: as many equal ranges as there are workgroups, so that ragged lengths end
+// together; a range may hold the end of one (sequence, head), whole ones, and the beginning of another. Few: pieces that end with their sequence. What is
+// not whole goes to the workspace and is merged by whoever finds all of it published (decode_tail.h says how that works without waiting or clearing).
 //
-// A workgroup's four wavefronts take turns at the pages. Both products are 16x16x32 matrix instructions whose operands are what a
+// A workgroup's wavefronts take turns at the pages. Both products are 16x16x32 matrix instructions whose operands are what a
 // page holds: S[key][column] = K q, then O[dim][column] += V^T P with the scores of a lane as they are, because the V plane
 // keeps the rows of a lane together.
 //
@@ -28,10 +32,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegBig = -1.0e30f;      // "no row seen yet": finite, so m - m never makes NaN
-constexpr int kWholePages = 16;          // as many are not worth a merge, ...
-constexpr int kMinPages = 2;             // ... and a wavefront has no fewer
-constexpr int kManyPages = 8;            // of a wavefront
-constexpr int kAhead4 = 2, kAhead2 = 4, kAheadPlain = 8;
+// Pages of a (sequence, head) that are not worth a merge (1 x 1000 rows, 16 pages: 10.4 us, cut in two 13.9), and those that a wavefront has
+// at least where it is cut (8 x 3000: 12.5 us, with 4 15.0).
+constexpr int kWholePages = 16, kMinPages = 2;
+// Pages of a wavefront from which on they are shared out in ranges (16 x 32768: 98 us, in pieces 103; 8 x 3000: 12.5, in ranges 18.1; 40 x 2000, 8
+// pages: 21.3, in ranges 26.9), and several are scored at once (below).
+constexpr int kManyPages = 8;
+// Planes of 4-bit pages, and KiB of bf16 ones, that a wavefront has asked for ahead. 4 bits, 8 columns: 16 x 32768 102.9 us, with 4 planes 105.5; 4
+// columns 98.7, with 4 101.5. bf16: 16 x 32768 318 us, with 4 KiB 366.
+constexpr int kAheadCoded = 2, kAheadPlain = 8;
 
 // A value from which nothing is worked out ahead of this place: what the compiler works out for all turns of a loop keeps its registers
 // through all of them.
@@ -208,8 +217,9 @@ __device__ __forceinline__ u32x4 only(bool mine, u32x4 x) { return (u32x4){mine 
 
 constexpr int kParamStride = 64 * 32 + 32;     // of a page's scales in LDS: the four pages of a read fall in distinct banks
 
-template <int D, int NP, int R, int TILES = 1>
+template <int D, int NP, int TILES = 1>
 struct Coded {
+  static constexpr int R = kAheadCoded;
   static constexpr int kGroups = D / 64, kSteps = D / 32, kLoads = D / 32;        // 16-byte loads of a plane's page
   static constexpr int kPages = NP, kTiles = TILES, kColumns = 16 / NP;       // kColumns: of a tile
   static constexpr bool kStash = kSteps * TILES > 4;                              // the query lies in LDS: there are no registers for it
@@ -492,8 +502,9 @@ struct Coded {
 };
 
 // ---- bf16 pages: softmax weights go in as a bf16 high part and a bf16 remainder (two products), which keeps 16 bits of them
-template <int D, int R, int TILES = 1>
+template <int D, int TILES = 1>
 struct Plain {
+  static constexpr int R = kAheadPlain;
   static constexpr int kSteps = D / 32, kLoads = D / 8, kPages = 1, kTiles = TILES, kColumns = 16, kLds = 16;
   static_assert(kLoads % R == 0, "a piece has its place among R in either plane");
   struct Pages {
@@ -798,7 +809,8 @@ __device__ __forceinline__ void attend(const Args& a, const int32_t* __restrict_
   for (int i = lane; i < parts; i += 64) put_u64(place(i) + slot.tag(wave), 0ull);       // a captured launch can be replayed
 }
 
-// Long: the form where a wavefront has many pages.
+// Long: the form where a wavefront has many pages, or as many as one step of it takes (1 x 1000: 9.5 us, a page at a time 10.5; but 24 x 5000, 5 pages:
+// 25.3, a page at a time 21.5).
 template <int D, int WAVES, typename Form, typename Long>
 __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(Args a, const int32_t* __restrict__ table) {
   __shared__ __attribute__((aligned(16))) Lds<D, WAVES, Long> lds;
@@ -822,7 +834,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(Args a, const int32
     if (ranges) piece = shares.piece_at(u, end, before);
     const int pages = piece.p1 - piece.p0;
     u += ranges ? pages : 1;
-    if (!std::is_same<Form, Long>::value && pages >= WAVES * kManyPages) attend<D, WAVES, Long>(a, table, piece, lds.red, lds.params);
+    const int each = (pages + WAVES - 1) / WAVES;
+    if (!std::is_same<Form, Long>::value && (each >= kManyPages || each == 4)) attend<D, WAVES, Long>(a, table, piece, lds.red, lds.params);
     else attend<D, WAVES, Form>(a, table, piece, lds.red, lds.params);
     __syncthreads();                                                     // what the merge has read is written again
   }
@@ -873,15 +886,15 @@ hipError_t launch_paged_attn(const PagedAttnView& v, void* workspace, unsigned l
   auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * p.waves), 0, s, a, v.table); };
   auto coded = [&](auto d, auto waves) {
     constexpr int D = decltype(d)::value, WAVES = decltype(waves)::value;
-    if (p.columns <= 4) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 4, kAhead4>>);
-    else if (p.columns <= 8) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 2, kAhead2>>);
-    else if (p.columns <= 16) go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 1, 2>>);
-    else go(&attn_kernel<D, WAVES, Coded<D, 1, 2, 2>, Coded<D, 1, 2, 2>>);
+    if (p.columns <= 4) go(&attn_kernel<D, WAVES, Coded<D, 1>, Coded<D, 4>>);
+    else if (p.columns <= 8) go(&attn_kernel<D, WAVES, Coded<D, 1>, Coded<D, 2>>);
+    else if (p.columns <= 16) go(&attn_kernel<D, WAVES, Coded<D, 1>, Coded<D, 1>>);
+    else go(&attn_kernel<D, WAVES, Coded<D, 1, 2>, Coded<D, 1, 2>>);
   };
   auto by_d = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (v.c.dtype != YOCO_INT4 && p.columns <= 16) go(&attn_kernel<D, 4, Plain<D, kAheadPlain>, Plain<D, kAheadPlain>>);
-    else if (v.c.dtype != YOCO_INT4) go(&attn_kernel<D, 4, Plain<D, kAheadPlain, 2>, Plain<D, kAheadPlain, 2>>);
+    if (v.c.dtype != YOCO_INT4 && p.columns <= 16) go(&attn_kernel<D, 4, Plain<D>, Plain<D>>);
+    else if (v.c.dtype != YOCO_INT4) go(&attn_kernel<D, 4, Plain<D, 2>, Plain<D, 2>>);
     else if (p.waves == 8) coded(d, std::integral_constant<int, 8>());
     else coded(d, std::integral_constant<int, 4>());
   };
