@@ -1,7 +1,7 @@
 // Rows into pages and back: the rotation to their positions, the 4-bit coding, and the order inside a page. Bound by memory where rows are
-// many, by the launch where they are few. One prompt of 32768 rows, 24:8 heads of 128 dimensions in bf16: into 4 bits with the queries 136 us (575 MB read
-// and written, 4.2 TB/s; a copy reaches 4.8), K and V alone 54 (3.2 TB/s: about 16 vector instructions a number to code it), into bf16 pages with the queries
-// 142 (4.7 TB/s); read back 36 us (4.7 TB/s). A row of each of 16 sequences: 4.2 us, read back 2.7.
+// many, by the launch where they are few. One prompt of 32768 rows, 24:8 heads of 128 dimensions in bf16: into 4 bits with the queries 126 us (575 MB read
+// and written, 4.6 TB/s; a copy reaches 4.8), K and V alone 45 (3.8 TB/s: the vector instructions of the angles and the coding; where nothing turns 36.5,
+// 4.7 TB/s), into bf16 pages with the queries 142 (4.7 TB/s); read back 36 us (4.8 TB/s). A row of each of 16 sequences: 4.0 us, read back 2.7.
 //
 // A workgroup has the 16 rows of a page that lie together in the operands (of which a call may bring fewer), and all heads of
 // them or a part. The angle of a pair at a position is a whole number of 2^-64 turns times the position, wrapped: exact wherever the
@@ -102,7 +102,7 @@ struct Group {
       most = max(most, opaque_bits(x[j]) & 0x7fffffffu);
     }
   }
-  template <int THREADS>                             // that hold the row of a head, side by side
+  template <int THREADS>                             // that hold the group, side by side
   __device__ __forceinline__ void join() {
     if (most >= 0x7f800000u) {                       // an infinity or a NaN: a range that is none
       lo = -INFINITY;
@@ -115,8 +115,8 @@ struct Group {
   __device__ __forceinline__ unsigned param() const {
 #pragma clang fp contract(off)
     const float range = hi - lo;
-    const unsigned base = f32_to_bf16(lo);
-    unsigned scale = f32_to_bf16(range * (float)(1.0 / 15.0));
+    const unsigned both = pack_bf16(range * (float)(1.0 / 15.0), lo), base = both >> 16;
+    unsigned scale = both & 0xffffu;
     if (scale < 0x0080u) scale = 0;                  // below the normal numbers: all of one value
     if (not_finite(range) || (scale & 0x7f80u) == 0x7f80u || (base & 0x7f80u) == 0x7f80u) return 0x7fc00000u;      // scale 0, minimum NaN
     return scale | (base << 16);
@@ -124,9 +124,10 @@ struct Group {
 };
 // The codes of 8 dimensions, 4 bits each, lowest dimension first. A number below 2^22 is rounded to the nearest whole one, half to even, by adding
 // 1.5 * 2^23, in whose lower bits it then stands; the upper ones are taken off for all 8 at once.
-__device__ __forceinline__ unsigned code8(const float (&x)[8], unsigned param) {
+__device__ __forceinline__ float steps_of(unsigned param) { return (param & 0xffffu) ? 1.f / __uint_as_float(param << 16) : 0.f; }
+__device__ __forceinline__ unsigned code8(const float (&x)[8], unsigned param, float inv) {
 #pragma clang fp contract(off)
-  const float s = __uint_as_float(param << 16), base = __uint_as_float(param & 0xffff0000u), inv = (param & 0xffffu) ? 1.f / s : 0.f;
+  const float base = __uint_as_float(param & 0xffff0000u);
   unsigned codes = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -171,15 +172,16 @@ __global__ void __launch_bounds__(256) append_kernel(AppendView a, int tiles, in
     const int64_t row = row_of(r);
     return h < keys ? (const S*)a.q + row * a.q_stride + (int64_t)h * D : h < values ? (const S*)a.k + row * a.k_stride + (int64_t)(h - keys) * D : (const S*)a.v + row * a.v_stride + (int64_t)(h - values) * D;
   };
-  int i = first * nr + slot;
+  // a slot has every kSlots-th of the heads' rows
+  const int dh = kSlots / nr, dr = kSlots - dh * nr;
+  int h = first + slot / nr, r = r0 + slot % nr;
   float x[8], y[8];
-  auto fetch = [&](int i, float(&x)[8], float(&y)[8]) {
-    const int h = i / nr;
-    const S* const p = source(h, r0 + i - h * nr);
+  auto fetch = [&](int h, int r, float(&x)[8], float(&y)[8]) {
+    const S* const p = source(h, r);
     load8(p + (h < values ? c0 : v0), x);
     load8(p + (h < values ? c1 : v1), y);
   };
-  if (i < last1 * nr) fetch(i, x, y);                                             // on their way while the angles are formed
+  if (h < last1) fetch(h, r, x, y);                                               // on their way while the angles are formed
   const int pairs = first < values ? a.rot / 2 : 0;
   for (int k = threadIdx.x; k < nr * pairs; k += 256) {
     const int r = k / pairs, p = k - r * pairs;
@@ -193,28 +195,47 @@ __global__ void __launch_bounds__(256) append_kernel(AppendView a, int tiles, in
   if (page >= a.c.n_pages) page = -1;
   const int base = (int)(at & (kPageRows - 1));
   auto place = [&](void* plane, int head) { return (char*)plane + ((int64_t)page * a.c.Hkv + head) * page_bytes(D, CODED ? YOCO_INT4 : YOCO_BF16); };
-  // the scales of a row's groups, from the pieces of all of its threads
-  auto scales = [&](const float(&x)[8], const float(&y)[8], int e0, int e1, unsigned(&param)[kGroups]) {
+  // The codes of a row, whose scales go to `to`. Where both pieces of a thread are of one group, the group is four threads'; else (keys that turn over
+  // more than half a head of 128) every thread has a part in both.
+  auto codes_of = [&](const float (&x)[8], const float (&y)[8], int e0, int e1, bool one, char* to, int row, unsigned& cx, unsigned& cy) {
+    Group gx, gy;
+    gx.see(x);
+    if (kGroups == 1 || one) {
+      gx.see(y);
+      gx.template join<4>();
+      const unsigned p = gx.param();
+      const float inv = steps_of(p);
+      cx = code8(x, p, inv);
+      cy = code8(y, p, inv);
+      if (th % 4 == 0) *(unsigned*)(to + param4_byte(row, th / 4 * 64, D)) = p;
+    } else {
+      gy.see(y);
+      unsigned p[2];
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      Group group;
-      if (kGroups == 1 || e0 / 64 == g) group.see(x);
-      if (kGroups == 1 || e1 / 64 == g) group.see(y);
-      group.template join<kThreads>();
-      param[g] = group.param();
+      for (int g = 0; g < 2; ++g) {
+        const bool in_x = e0 / 64 == g, in_y = e1 / 64 == g;
+        Group group;
+        group.lo = fminf(in_x ? gx.lo : INFINITY, in_y ? gy.lo : INFINITY);
+        group.hi = fmaxf(in_x ? gx.hi : -INFINITY, in_y ? gy.hi : -INFINITY);
+        group.most = max(in_x ? gx.most : 0u, in_y ? gy.most : 0u);
+        group.template join<8>();
+        p[g] = group.param();
+      }
+      const unsigned px = e0 < 64 ? p[0] : p[1], py = e1 < 64 ? p[0] : p[1];
+      cx = code8(x, px, steps_of(px));
+      cy = code8(y, py, steps_of(py));
+      if (th < 2) *(unsigned*)(to + param4_byte(row, th * 64, D)) = th ? p[1] : p[0];
     }
   };
-  auto of = [&](const unsigned(&param)[kGroups], int e) { return kGroups > 1 && e >= 64 ? param[kGroups - 1] : param[0]; };
+  const bool one = a.neighbours || a.rot <= D / 2;
   // V of row r of the page's 16, into the page or, of all 16, into LDS in the page's order: 4 rows side by side
   auto put_v = [&](int h, int r, const float(&x)[8], const float(&y)[8]) {
     char* const to = place(a.c.v, h);
     unsigned char* const lds = turn[slot / kTileRows];
     const int quad = r / 4 * 16, i4 = r % 4;
     if constexpr (CODED) {
-      unsigned param[kGroups];
-      scales(x, y, v0, v1, param);
-      const unsigned lo = code8(x, of(param, v0)), hi = code8(y, of(param, v1));
-      if (th < kGroups) *(unsigned*)(to + param4_byte(base + r, th * 64, D)) = of(param, th * 64);
+      unsigned lo, hi;
+      codes_of(x, y, v0, v1, true, to, base + r, lo, hi);
       const unsigned even = (lo & 0x0f0f0f0fu) | (hi & 0x0f0f0f0fu) << 4, odd = (lo >> 4 & 0x0f0f0f0fu) | (hi & 0xf0f0f0f0u);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -237,10 +258,14 @@ __global__ void __launch_bounds__(256) append_kernel(AppendView a, int tiles, in
     }
   };
 
-  for (; i < last1 * nr; i += kSlots) {
-    const int h = i / nr, r = r0 + i - h * nr;
+  while (h < last1) {
     float nx[8], ny[8];
-    if (i + kSlots < last1 * nr) fetch(i + kSlots, nx, ny);
+    int h2 = h + dh, r2 = r + dr;
+    if (r2 >= r0 + nr) {
+      r2 -= nr;
+      ++h2;
+    }
+    if (h2 < last1) fetch(h2, r2, nx, ny);
     if (h < values) rotate(x, y, c0, c1, a.rot, a.neighbours, cs[r]);
     if (h < keys) {
       S* const to = (S*)a.q_out + (row_of(r) * a.Hq + h) * D;
@@ -252,17 +277,18 @@ __global__ void __launch_bounds__(256) append_kernel(AppendView a, int tiles, in
       } else {
         char* const to = place(a.c.k, h - keys);
         if constexpr (CODED) {
-          unsigned param[kGroups];
-          scales(x, y, c0, c1, param);
-          *(unsigned*)(to + k4_byte(base + r, c0, D)) = code8(x, of(param, c0));
-          *(unsigned*)(to + k4_byte(base + r, c1, D)) = code8(y, of(param, c1));
-          if (th < kGroups) *(unsigned*)(to + param4_byte(base + r, th * 64, D)) = of(param, th * 64);
+          unsigned cx, cy;
+          codes_of(x, y, c0, c1, one, to, base + r, cx, cy);
+          *(unsigned*)(to + k4_byte(base + r, c0, D)) = cx;
+          *(unsigned*)(to + k4_byte(base + r, c1, D)) = cy;
         } else {
           store8((bf16_t*)to + k16_at(base + r, c0, D), x);
           store8((bf16_t*)to + k16_at(base + r, c1, D), y);
         }
       }
     }
+    h = h2;
+    r = r2;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       x[j] = nx[j];
@@ -272,7 +298,7 @@ __global__ void __launch_bounds__(256) append_kernel(AppendView a, int tiles, in
   if (!whole || page < 0) return;
   int h0 = first > values ? first - values : 0;
   auto fetch_v = [&](int h0) {
-    if (h0 + slot / kTileRows < last - values) fetch((values + h0 + slot / kTileRows) * kTileRows + slot % kTileRows, x, y);
+    if (h0 + slot / kTileRows < last - values) fetch(values + h0 + slot / kTileRows, slot % kTileRows, x, y);
   };
   fetch_v(h0);
   for (; h0 < last - values; h0 += kSlots / kTileRows) {
