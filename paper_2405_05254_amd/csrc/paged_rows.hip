@@ -1,7 +1,7 @@
 // Rows into pages and back: the rotation to their positions, the 4-bit coding, and the order inside a page. Bound by memory where rows are
 // many, by the launch where they are few. One prompt of 32768 rows, 24:8 heads of 128 dimensions in bf16: into 4 bits with the queries 126 us (575 MB read
-// and written, 4.6 TB/s; a copy reaches 4.8), K and V alone 45 (3.8 TB/s: the vector instructions of the angles and the coding; where nothing turns 36.5,
-// 4.7 TB/s), into bf16 pages with the queries 142 (4.7 TB/s); read back 36 us (4.8 TB/s). A row of each of 16 sequences: 4.0 us, read back 2.7.
+// and written, 4.6 TB/s; a copy reaches 4.8), K and V alone 44 (3.9 TB/s: the vector instructions of the angles and the coding; where nothing turns 36.5,
+// 4.7 TB/s), into bf16 pages with the queries 142 (4.7 TB/s); read back 36 us (4.8 TB/s). A row of each of 16 sequences: 3.9 us, read back 2.7.
 //
 // A workgroup has the 16 rows of a page that lie together in the operands (of which a call may bring fewer), and all heads of
 // them or a part. The angle of a pair at a position is a whole number of 2^-64 turns times the position, wrapped: exact wherever the
@@ -47,13 +47,20 @@ __device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {
   *(u32x4*)p = (u32x4){pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
 }
 
-// Cosine and sine of pair p at a position: the upper 32 bits of the phase are a signed part of a turn.
+// Cosine and sine of a pair at a position: the upper 32 bits of the phase are a signed part of a turn. Whole quarters are taken off it as they are, in
+// integers; of what is left, an eighth of a turn at most, the power series' next terms are below 2^-31.
 __device__ __forceinline__ float2 turn_of(uint64_t turns, int64_t pos) {
-  const int32_t part = (int32_t)(((uint64_t)pos * turns) >> 32);
-  const float a = (float)part * (float)(6.283185307179586 / 4294967296.0);
-  float s, c;
-  sincosf(a, &s, &c);
-  return make_float2(c, s);
+  const unsigned part = (unsigned)(((uint64_t)pos * turns) >> 32), quarter = (part + 0x20000000u) >> 30;
+  const float a = (float)(int32_t)(part - (quarter << 30)) * (float)(6.283185307179586 / 4294967296.0), z = a * a;
+  float s = fmaf(z, 1.f / 362880.f, -1.f / 5040.f), c = fmaf(z, -1.f / 3628800.f, 1.f / 40320.f);
+  s = fmaf(z, s, 1.f / 120.f);
+  c = fmaf(z, c, -1.f / 720.f);
+  s = fmaf(z, s, -1.f / 6.f);
+  c = fmaf(z, c, 1.f / 24.f);
+  s = fmaf(a * z, s, a);
+  c = fmaf(z, fmaf(z, c, -0.5f), 1.f);
+  const float x = quarter & 1u ? s : c, y = quarter & 1u ? c : s;
+  return make_float2(__uint_as_float(__float_as_uint(x) ^ ((quarter + 1u) & 2u) << 30), __uint_as_float(__float_as_uint(y) ^ (quarter & 2u) << 30));
 }
 
 // Products and sums rounded apart, as the formulas print them.
