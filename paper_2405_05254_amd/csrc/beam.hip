@@ -251,8 +251,8 @@ __global__ void __launch_bounds__(64 * kMaxBeams) select_merge_kernel(SelectView
 }
 
 // 8-logit pieces a thread: as few as leave a row no more than 32 chunks to merge and the chip no more than about 1000 workgroups. A row of a
-// few thousand logits is done soonest with 1 (4 beams x 32000: 7.0 us, with 4 8.3), many long rows with 4 (128 x 128000 float32: 21.5 us, with
-// 1 35 and with 2 25; 8 would be 23.7).
+// few thousand logits is done soonest with 1 (4 beams x 32000: 6.9 us, with 4 8.3), many long rows with 4 (128 x 128000 float32: 21.2 us, with
+// 1 30.6 and with 2 23.5; 8 took 23.7).
 int select_pieces(int rows, int V) {
   for (int vecs = 1; vecs < 4; vecs *= 2)
     if ((V + 2048 * vecs - 1) / (2048 * vecs) <= 32 && (int64_t)rows * V <= (int64_t)2048 * vecs * 1024) return vecs;
@@ -262,7 +262,7 @@ int select_chunks(int vecs, int V) { return ((V + 7) / 8 + 1 + vecs * 256 - 1) /
 
 // ---- states in the order of their parents, in place: a thread has the same 16 bytes of all beams, and reads before it writes.
 // Beam w's come from from[w] and go to into[w] where moves[w], of n pieces of 16 bytes. A beam that stays is one whose window of memory is empty:
-// its loads and stores go nowhere, and none of the others waits for a branch (26 states of 2 x 8 beams x 2 MiB: 382 us with branches, 259 without).
+// its loads and stores go nowhere, and none of the others waits for a branch (26 states of 2 x 8 beams x 2 MiB: 382 us with branches, 267 without).
 template <int WM>
 __device__ __forceinline__ void move_pieces(u32x4* const (&from)[WM], u32x4* const (&into)[WM], const bool (&moves)[WM], int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256; i < n; i += (int64_t)gridDim.x * 256) {
